@@ -387,6 +387,150 @@ ABSB_API int absb_head_recall(const absb_layer* layer, const absb_batch* batch, 
 ABSB_API int absb_assign_block_sizes(int32_t n_samples, int32_t n_heads, int32_t n_cand, const float* recall_host,
                                      const int32_t* cand, double tau, int32_t* block_size_out, double* mean_out);
 
+/* ---- Around the cache: the rows of a step, rotary positions, dense attention of new rows ----
+ *
+ * A server's step brings every request of the batch some new tokens (none, one, a chunk of a prompt).
+ * The entry points below say where they go, write their keys and values, and attend from them over
+ * everything their requests hold, on the same paged caches and page tables as the rest of the library.
+ * They read layer->num_q_heads, num_kv_heads, head_dim, page_size, dtype, the K/V strides (kv_stride_tok
+ * at most 2^28) and sm_scale; block sizes and the selection policy do not matter to them
+ * (layer->block_size may be NULL).  Lengths may be 0 here.
+ *
+ * "Rows": the new tokens of all requests side by side, request b's at [row_off[b], row_off[b+1]).  They
+ * are the LAST tokens of their context: with n_b rows and length L_b (which counts them), row
+ * row_off[b] + i is token L_b - n_b + i. */
+typedef struct absb_rows {
+  const int32_t* row_off_host; /* host [Bt+1]: 0 = off[0] <= off[1] <= ...; off[b+1] - off[b] <= L_b   */
+  const int32_t* row_off;      /* device [Bt+1], same values                                      */
+} absb_rows;
+
+/* Free physical pages: entries head <= i < tail of an endless list, entry i kept at pages[i % capacity]. */
+typedef struct absb_page_ring {
+  int32_t* pages;            /* device [capacity]                                               */
+  int32_t capacity;          /* >= the number of physical pages, so that the ring never overflows */
+  const int64_t* cursors;    /* device [4]: head, tail (0 <= tail - head <= capacity); [2] is not read, [3] = 0 */
+  int64_t* cursors_out;      /* device [4]: head, tail after the call; [2] = pages that were missing;
+                                [3] = 0.  May be `cursors`.  [3] must be zero when the call starts. */
+} absb_page_ring;
+
+/* The rows of a step and where they go, from the requests' lengths before and after it, on the device:
+ * nothing is read from the host's twins, so a captured call follows the lengths that it finds.
+ *   lens_before [Bt], batch->seq_lens [Bt] : lengths before and after.  A request with more tokens after
+ *             than before grows by n_b = after - before rows; one with fewer shrinks (to 0: it has
+ *             finished), n_b = 0.  Negative lengths count as 0.
+ *   page_table [Bt][batch->pt_stride] : the tables.  With a ring, a request that grows beyond its
+ *             ceil(before/P) pages takes the ones it needs from the ring, request after request and page
+ *             after page, and one that shrinks gives those beyond ceil(after/P) back in the same order
+ *             (its entries stay as they were; pages given back are free from the next call on).  Without
+ *             one (ring NULL) the tables are complete and only read.
+ *   row_off [Bt+1] i32  : prefix sums of n_b (any larger than max_rows included)
+ *   row_pos [max_rows] i32, row_slot [max_rows] i64 : of every row, its position in its request and its
+ *             slot in the cache, page * P + position % P.  Rows behind the last one get position 0 and
+ *             slot -1.
+ * All or nothing: if the ring holds too few free pages, or a table row is too short for its request's
+ * pages, then no table, no page and no cursor changes, every row_slot is -1 and cursors_out[2] (written
+ * with a ring only) says how many pages were missing.  Without a ring, rows beyond the table's width get
+ * slot -1.  Sums of rows and of pages must stay below 2^31; batch is at most 65535.  Reads batch->batch,
+ * pt_stride and seq_lens, and layer->page_size. */
+ABSB_API int absb_map_rows(const absb_layer* layer, const absb_batch* batch, const int32_t* lens_before,
+                           int32_t* page_table, const absb_page_ring* ring, int32_t max_rows, int32_t* row_off,
+                           int32_t* row_pos, int64_t* row_slot, void* stream);
+
+/* Rotary positions.  A head's first rot_dim channels are taken as rot_dim/2 pairs (x, y); pair i of a
+ * token at position p turns by the angle p * f_i:  (x, y) -> amplitude * (x cos - y sin, x sin + y cos).
+ * The other channels pass.  Which channels make pair i: */
+typedef enum absb_rope_layout {
+  ABSB_ROPE_HALVES = 0, /* i and i + rot_dim/2 */
+  ABSB_ROPE_PAIRS = 1   /* 2i and 2i + 1       */
+} absb_rope_layout;
+/* How frequencies follow from base^(-2i/rot_dim) for contexts longer than a model was trained on: */
+typedef enum absb_rope_scaling {
+  ABSB_ROPE_PLAIN = 0,    /* as they are                                                          */
+  ABSB_ROPE_LINEAR = 1,   /* all divided by `factor` (positions interpolated)                      */
+  ABSB_ROPE_BASE = 2,     /* base * factor^(rot_dim/(rot_dim-2)) in place of base (rot_dim > 2): the lowest
+                             frequency is divided by `factor`, the highest stays                      */
+  ABSB_ROPE_BY_TURNS = 3  /* by how often a pair turns within original_len tokens: at most low_turns:
+                             divided by `factor`; at least high_turns: as they are; between, the two
+                             blended in proportion to the turns                                     */
+} absb_rope_scaling;
+typedef struct absb_rope {
+  int32_t rot_dim;        /* even, 2..128                                                        */
+  int32_t layout;         /* absb_rope_layout                                                    */
+  int32_t scaling;        /* absb_rope_scaling; read by absb_rope_frequencies only, as are the next five */
+  double base;            /* > 1                                                                 */
+  double factor;          /* >= 1; read unless PLAIN                                              */
+  double original_len;    /* > 0; BY_TURNS only, as are the next two                               */
+  double low_turns, high_turns; /* 0 <= low < high                                                */
+  float amplitude;        /* of the rotated channels; 0 selects 1                                  */
+} absb_rope;
+
+/* Host only: freq_host [rot_dim/2] f64, radians per position. */
+ABSB_API int absb_rope_frequencies(const absb_rope* rope, double* freq_host);
+
+/* Rotates queries and keys to their positions and writes keys and values into the paged caches.
+ *   row_pos [n_rows] i32, row_slot [n_rows] i64 : as absb_map_rows writes them.  A row whose slot is negative
+ *             has its query rotated and nothing stored.  Two rows with one slot: either is kept.
+ *   freq [rot_dim/2] f64 device : radians per position, |freq| < 2^32.  Angles are exact to 2^-32 turns + position *
+ *             2^-52 |freq| at any position.
+ *   q [n_rows][Hq][d], k, v [n_rows][Hkv][d] : rows q_stride, k_stride, v_stride elements apart (multiples of 8, so that the
+ *             three may lie side by side in one projection's output), 16-byte aligned.
+ *   q_out [n_rows][Hq][d] : rotated queries; may be q itself when q_stride is Hq*d, and must not overlap
+ *             q, k or v otherwise.  q and q_out both NULL: keys and values only.  k and v both NULL: queries only.
+ * Products and sums in binary32, one rounding to the K/V type; v is copied bit for bit. */
+ABSB_API int absb_rotate_store(const absb_layer* layer, const absb_rope* rope, int32_t n_rows, const int32_t* row_pos,
+                               const int64_t* row_slot, const double* freq, const void* q, int64_t q_stride, void* q_out,
+                               const void* k, int64_t k_stride, const void* v, int64_t v_stride, void* k_cache,
+                               void* v_cache, void* stream);
+
+/* What a row sees and how a score is changed.  Row at position i of request b sees key j if
+ *   j < L_b,  j <= i or j < prefix_lens[b],  i - j < window (if set),  and  j >= doc_start[row] (if set).
+ * score = sm_scale * q.k;  then softcap * tanh(score / softcap) (if set);  then - slopes[head] * |i - j| (if
+ * set).  All zero and NULL: causal attention.  A row that sees nothing yields out = 0, lse = -inf. */
+typedef struct absb_score_opts {
+  float softcap;              /* 0 = none, else > 0                                              */
+  int32_t window;             /* 0 = none, else >= 1: tokens a row sees up to and including itself      */
+  const float* slopes;        /* device [Hq] or NULL                                             */
+  const int32_t* prefix_lens; /* device [Bt] or NULL: tokens that all rows of a request see            */
+  const int32_t* doc_start;   /* device [rows] or NULL: first token of the row's document              */
+} absb_score_opts;
+
+/* Groups of consecutive requests that share their first tokens, whole pages of them: requests
+ * [first[g], first[g+1]) have the same first len[g]/P entries in their page-table rows. */
+typedef struct absb_shared_prefix {
+  int32_t groups;               /* >= 1                                                          */
+  const int32_t* first_host;    /* host [groups+1]: 0 = first[0] <= first[1] <= ... = Bt              */
+  const int32_t* len_host;      /* host [groups]: shared tokens; a multiple of the page size, 0 allowed;
+                                   every request's L_b - n_b >= its group's len                     */
+  const int32_t* first;         /* device [groups+1], same values                                */
+  const int32_t* len;           /* device [groups], same values                                  */
+} absb_shared_prefix;
+
+/* Workspace of the two entry points below for these rows and any options (`shared` NULL: of
+ * absb_attend_rows).  May be 0.  Nothing in it needs initialisation or survives a call; calls that share one must
+ * be ordered on one stream.  Reads host fields only. */
+ABSB_API int absb_attend_workspace(const absb_layer* layer, const absb_batch* batch, const absb_rows* rows,
+                                   const absb_shared_prefix* shared, size_t* workspace_bytes);
+
+/* Dense attention of every request's rows over its context in the paged caches, the rows' own keys and
+ * values included (absb_rotate_store has written them).  Prompts, chunks of prompts, single tokens, any
+ * mixture.
+ *   q, out [rows][Hq][d] (16-byte aligned; out may be q), lse [rows][Hq] f32 optional (NULL ok)
+ *   opts : NULL = causal attention and nothing else
+ * Reads batch->batch, seq_lens(_host), page_table and pt_stride (>= ceil(max L_b / P)).  Slots beyond a
+ * context may hold anything; the tokens of a context must be finite, also those that the row does not see.
+ * Accumulation, maxima and sums are binary32; the softmax weights enter the product with V rounded to the K/V
+ * type, their sum is taken before rounding. */
+ABSB_API int absb_attend_rows(const absb_layer* layer, const absb_batch* batch, const absb_rows* rows, const void* q,
+                              const void* k_cache, const void* v_cache, void* out, float* lse,
+                              const absb_score_opts* opts, void* workspace, size_t workspace_bytes, void* stream);
+
+/* absb_attend_rows for a batch whose groups of requests share a prefix: the same results up to the order of
+ * sums, but the shared keys and values are read once for all rows of a group. */
+ABSB_API int absb_attend_shared(const absb_layer* layer, const absb_batch* batch, const absb_rows* rows,
+                                const absb_shared_prefix* shared, const void* q, const void* k_cache,
+                                const void* v_cache, void* out, float* lse, const absb_score_opts* opts,
+                                void* workspace, size_t workspace_bytes, void* stream);
+
 /* Measurement helper, not a step of the method: reads `bytes` (a multiple of 16; the tail is
  * ignored) of the device buffer `src` (16-byte aligned) once with 128-bit loads and discards them.
  * Timing it gives the practical streaming-read ceiling of the device, against which the attention

@@ -21,6 +21,8 @@ LIB_PATH = os.environ.get("ABSB_LIB") or os.path.join(_HERE, "libabsb.so")
 F16, BF16 = 0, 1
 REPR_MEAN, REPR_MINMAX = 0, 1
 SELECT_GROUP, SELECT_PER_QUERY_HEAD, SELECT_GROUP_MAX = 0, 1, 2
+ROPE_HALVES, ROPE_PAIRS = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_BY_TURNS = 0, 1, 2, 3
 STEP_AUTO, STEP_PIPELINED, STEP_UNITS, STEP_PER_STAGE = 0, 1, 2, 3
 
 OK, ERR_NULL, ERR_BAD_SHAPE, ERR_BAD_BLOCK_SIZE, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_HIP = 0, -1, -2, -3, -4, -5, -6
@@ -29,7 +31,8 @@ STATIC_WORKSPACE_BYTES = 16 << 20
 
 EXPORTS = ("absb_plan", "absb_step_form_used", "absb_status_offset", "absb_workspace_init", "absb_build_centroids", "absb_score", "absb_topk", "absb_sparse_decode",
            "absb_decode_fused", "absb_tail_init", "absb_append_token", "absb_head_recall", "absb_assign_block_sizes", "absb_stream_read",
-           "absb_strerror", "absb_decode_fused_static")
+           "absb_strerror", "absb_decode_fused_static", "absb_map_rows", "absb_rope_frequencies", "absb_rotate_store",
+           "absb_attend_workspace", "absb_attend_rows", "absb_attend_shared")
 
 
 class AbsbError(RuntimeError):
@@ -60,6 +63,30 @@ class _Batch(C.Structure):
                 ("cap_lens_host", C.c_void_p), ("qmin", C.c_void_p), ("opts", _Opts)]
 
 
+class _Rows(C.Structure):
+    _fields_ = [("row_off_host", C.c_void_p), ("row_off", C.c_void_p)]
+
+
+class _Ring(C.Structure):
+    _fields_ = [("pages", C.c_void_p), ("capacity", C.c_int32), ("cursors", C.c_void_p), ("cursors_out", C.c_void_p)]
+
+
+class _Rope(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("layout", C.c_int32), ("scaling", C.c_int32), ("base", C.c_double),
+                ("factor", C.c_double), ("original_len", C.c_double), ("low_turns", C.c_double),
+                ("high_turns", C.c_double), ("amplitude", C.c_float)]
+
+
+class _ScoreOpts(C.Structure):
+    _fields_ = [("softcap", C.c_float), ("window", C.c_int32), ("slopes", C.c_void_p), ("prefix_lens", C.c_void_p),
+                ("doc_start", C.c_void_p)]
+
+
+class _Shared(C.Structure):
+    _fields_ = [("groups", C.c_int32), ("first_host", C.c_void_p), ("len_host", C.c_void_p), ("first", C.c_void_p),
+                ("len", C.c_void_p)]
+
+
 _lib = None
 
 # Argument types of the entry points: with them declared, integers, None, byref() records and c_void_p
@@ -81,6 +108,12 @@ _ARGTYPES = {
     "absb_append_token": [_REC, _REC, _P, _P, _P, _P, _P, _P, _P],
     "absb_head_recall": [_REC, _REC, _P, _P, _P, _P],
     "absb_stream_read": [_P, C.c_size_t, _P, _P],
+    "absb_map_rows": [_REC, _REC, _P, _P, _REC, C.c_int32, _P, _P, _P, _P],
+    "absb_rope_frequencies": [_REC, _P],
+    "absb_rotate_store": [_REC, _REC, C.c_int32, _P, _P, _P, _P, C.c_int64, _P, _P, C.c_int64, _P, C.c_int64, _P, _P, _P],
+    "absb_attend_workspace": [_REC, _REC, _REC, _REC, _P],
+    "absb_attend_rows": [_REC, _REC, _REC, _P, _P, _P, _P, _P, _REC, _P, C.c_size_t, _P],
+    "absb_attend_shared": [_REC, _REC, _REC, _REC, _P, _P, _P, _P, _P, _REC, _P, C.c_size_t, _P],
 }
 
 
@@ -285,6 +318,101 @@ _BATCH_TENSORS = frozenset(("seq_lens", "page_table", "cent_off", "budget", "qmi
 _BATCH_FIELDS = (*_BATCH_HOST_ARRAYS, *_BATCH_TENSORS, "pt_stride")
 
 
+class _Record:
+    """Host description whose C record is built once per set of field values (any assignment drops it).  Tensors are
+    held by address: one that is resized in place has to be assigned again."""
+
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        if not name.startswith("_"):
+            object.__setattr__(self, "_c", None)
+
+    def c(self):
+        rec = getattr(self, "_c", None)
+        if rec is None:
+            rec = self._make()      # (host arrays that it points into are kept on the record itself)
+            object.__setattr__(self, "_c", rec)
+        return rec
+
+
+@dataclass
+class Rows(_Record):
+    """A step's new tokens (mirrors absb_rows): request b owns rows [row_off[b], row_off[b+1]), the last of its context.
+    `row_off_host` is a sequence of int, `row_off` the same values as an int32 device tensor."""
+    row_off_host: Sequence[int]
+    row_off: object = None
+
+    def _make(self):
+        a, at = _i32_host(self.row_off_host)
+        rec = _Rows(at, _ptr(self.row_off))
+        rec._arrays = (a,)
+        return rec
+
+
+@dataclass
+class PageRing(_Record):
+    """Free physical pages (mirrors absb_page_ring): `pages` int32 device tensor, one place per physical page; `cursors`
+    int64 device tensor [4] = head, tail, -, 0."""
+    pages: object
+    cursors: object
+
+    def _make(self):
+        return _Ring(_ptr(self.pages), self.pages.numel(), _ptr(self.cursors), _ptr(self.cursors))
+
+
+@dataclass
+class Rope(_Record):
+    """Rotary positions (mirrors absb_rope)."""
+    rot_dim: int = 128
+    layout: int = ROPE_HALVES
+    base: float = 10000.0
+    scaling: int = ROPE_PLAIN
+    factor: float = 1.0
+    original_len: float = 0.0
+    low_turns: float = 0.0
+    high_turns: float = 0.0
+    amplitude: float = 0.0
+
+    def _make(self):
+        return _Rope(int(self.rot_dim), int(self.layout), int(self.scaling), float(self.base), float(self.factor),
+                     float(self.original_len), float(self.low_turns), float(self.high_turns), float(self.amplitude))
+
+
+@dataclass
+class ScoreOpts(_Record):
+    """What a row sees and how its scores are changed (mirrors absb_score_opts).  `slopes` f32 [Hq], `prefix_lens` int32
+    [Bt], `doc_start` int32 [rows]: device tensors or None."""
+    softcap: float = 0.0
+    window: int = 0
+    slopes: object = None
+    prefix_lens: object = None
+    doc_start: object = None
+
+    def _make(self):
+        return _ScoreOpts(float(self.softcap), int(self.window), _ptr(self.slopes), _ptr(self.prefix_lens), _ptr(self.doc_start))
+
+
+@dataclass
+class SharedPrefix(_Record):
+    """Groups of consecutive requests with the same first pages (mirrors absb_shared_prefix): `first_host` [groups+1] and
+    `len_host` [groups] are sequences of int, `first` and `length` the same values as int32 device tensors."""
+    first_host: Sequence[int]
+    len_host: Sequence[int]
+    first: object = None
+    length: object = None
+
+    def _make(self):
+        a, a_at = _i32_host(self.first_host)
+        n, n_at = _i32_host(self.len_host)
+        rec = _Shared(len(n), a_at, n_at, _ptr(self.first), _ptr(self.length))
+        rec._arrays = (a, n)
+        return rec
+
+
+def _rec(r):
+    return None if r is None else C.byref(r.c())
+
+
 @dataclass
 class PlanResult:
     cent_off: np.ndarray       # int32 [Bt*Hkv+1]
@@ -404,6 +532,72 @@ def absb_assign_block_sizes(recall: np.ndarray, candidates: Sequence[int], tau: 
                                           C.c_double(tau), out.ctypes.data_as(C.c_void_p),
                                           mean.ctypes.data_as(C.c_void_p)), "absb_assign_block_sizes")
     return out, mean
+
+
+def absb_map_rows(layer: Layer, batch: Batch, lens_before, page_table, row_off, row_pos, row_slot, ring: PageRing = None,
+                  cursors_out=None, stream=None) -> None:
+    """`row_pos` and `row_slot` are as long as the most rows that the step may have; `cursors_out` None: in place."""
+    cl, cb = layer.c(), batch.c()
+    rec = None
+    if ring is not None:
+        rec = ring.c()
+        if cursors_out is not None:
+            rec = _Ring.from_buffer_copy(rec)
+            rec.cursors_out = _ptr(cursors_out)
+        rec = C.byref(rec)
+    if row_pos.numel() != row_slot.numel():
+        raise AbsbError(ERR_BAD_SHAPE, "absb_map_rows")
+    _check(load().absb_map_rows(C.byref(cl), C.byref(cb), _ptr(lens_before), _ptr(page_table), rec, row_pos.numel(), _ptr(row_off),
+                                _ptr(row_pos), _ptr(row_slot), _stream(stream)), "absb_map_rows")
+
+
+def absb_rope_frequencies(rope: Rope) -> np.ndarray:
+    """Radians per position, float64 [rot_dim/2]."""
+    out = np.zeros(64, np.float64)
+    _check(load().absb_rope_frequencies(_rec(rope), out.ctypes.data), "absb_rope_frequencies")
+    return out[:int(rope.rot_dim) // 2].copy()
+
+
+def _rows_of_heads(t, heads: int, where: str) -> int:
+    """Row stride of a [rows][heads][d] tensor whose heads and channels are dense (None: 0)."""
+    if t is None:
+        return 0
+    if t.dim() != 3 or t.shape[1] != heads or t.stride(2) != 1 or t.stride(1) != t.shape[2]:
+        raise AbsbError(ERR_BAD_SHAPE, where)
+    return t.stride(0) if t.shape[0] > 1 else heads * t.shape[2]
+
+
+def absb_rotate_store(layer: Layer, rope: Rope, row_pos, row_slot, freq, q=None, q_out=None, k=None, v=None, k_cache=None,
+                      v_cache=None, stream=None) -> None:
+    """q, k, v: [rows][heads][128], rows any multiple of 8 elements apart (views of one projection's output, say)."""
+    cl, where = layer.c(), "absb_rotate_store"
+    qs, ks, vs = (_rows_of_heads(t, h, where) for t, h in ((q, cl.num_q_heads), (k, cl.num_kv_heads), (v, cl.num_kv_heads)))
+    n = row_pos.numel()
+    if any(t is not None and t.shape[0] != n for t in (q, q_out, k, v)) or (q_out is not None and not q_out.is_contiguous()):
+        raise AbsbError(ERR_BAD_SHAPE, where)
+    _check(load().absb_rotate_store(C.byref(cl), _rec(rope), n, _ptr(row_pos), _ptr(row_slot), _ptr(freq), _ptr(q), qs, _ptr(q_out),
+                                    _ptr(k), ks, _ptr(v), vs, _ptr(k_cache), _ptr(v_cache), _stream(stream)), where)
+
+
+def absb_attend_workspace(layer: Layer, batch: Batch, rows: Rows, shared: SharedPrefix = None) -> int:
+    cl, cb = layer.c(), batch.c()
+    n = C.c_size_t(0)
+    _check(load().absb_attend_workspace(C.byref(cl), C.byref(cb), _rec(rows), _rec(shared), C.byref(n)), "absb_attend_workspace")
+    return int(n.value)
+
+
+def absb_attend_rows(layer: Layer, batch: Batch, rows: Rows, q, k_cache, v_cache, out, lse=None, opts: ScoreOpts = None,
+                     workspace=None, stream=None) -> None:
+    cl, cb = layer.c(), batch.c()
+    _check(load().absb_attend_rows(C.byref(cl), C.byref(cb), _rec(rows), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(out), _ptr(lse),
+                                   _rec(opts), _ptr(workspace), _nbytes(workspace), _stream(stream)), "absb_attend_rows")
+
+
+def absb_attend_shared(layer: Layer, batch: Batch, rows: Rows, shared: SharedPrefix, q, k_cache, v_cache, out, lse=None,
+                       opts: ScoreOpts = None, workspace=None, stream=None) -> None:
+    cl, cb = layer.c(), batch.c()
+    _check(load().absb_attend_shared(C.byref(cl), C.byref(cb), _rec(rows), _rec(shared), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(out),
+                                     _ptr(lse), _rec(opts), _ptr(workspace), _nbytes(workspace), _stream(stream)), "absb_attend_shared")
 
 
 def absb_stream_read(src, sink, stream=None) -> None:

@@ -34,6 +34,8 @@ _SOURCES = {
     "shared.hip": ["-ffp-contract=off"],   # likewise
     "small.hip": ["-ffp-contract=off"],    # likewise
     "util.hip": [],
+    "rows.hip": [],
+    "attend.hip": [],
 }
 
 

@@ -4,7 +4,9 @@
 #include <cmath>
 #include <mutex>
 
+#include "attend.h"
 #include "common.h"
+#include "rows.h"
 
 namespace absb {
 
@@ -305,6 +307,130 @@ static int check_ws(const void* ws, size_t have, size_t need) {
   return ABSB_OK;
 }
 
+// What the entry points around the cache read of a layer.
+static int check_dense_layer(const absb_layer* layer) {
+  if (!layer) return ABSB_ERR_NULL;
+  if (layer->head_dim != ABSB_HEAD_DIM) return ABSB_ERR_UNSUPPORTED;
+  if (layer->dtype != ABSB_F16 && layer->dtype != ABSB_BF16) return ABSB_ERR_UNSUPPORTED;
+  const int Hq = layer->num_q_heads, Hkv = layer->num_kv_heads;
+  if (Hq < 1 || Hkv < 1 || Hq % Hkv != 0) return ABSB_ERR_BAD_SHAPE;
+  if (Hq / Hkv > ABSB_MAX_GROUP || Hkv > ABSB_MAX_KV_HEADS) return ABSB_ERR_UNSUPPORTED;
+  const int P = layer->page_size;
+  if (!is_pow2(P) || P < 8 || P > 65536) return ABSB_ERR_BAD_SHAPE;
+  const int64_t sp = layer->kv_stride_page, sh = layer->kv_stride_head, st = layer->kv_stride_tok;
+  if (sp <= 0 || sh <= 0 || st < ABSB_HEAD_DIM || (sp % 8) || (sh % 8) || (st % 8)) return ABSB_ERR_BAD_SHAPE;
+  if (st > (int64_t(1) << 28)) return ABSB_ERR_UNSUPPORTED;
+  if (!(layer->sm_scale >= 0.0f) || std::isinf(layer->sm_scale)) return ABSB_ERR_BAD_SHAPE;
+  return ABSB_OK;
+}
+
+// Owners of a phase, as the host sees them: rows (tokens), keys that a tile of theirs can see at most and on average.
+struct PhaseSums {
+  int64_t tiles = 0, max_rows = 0;
+  double keys = 0;  // over tiles: keys on average
+  int64_t max_keys = 0;
+};
+
+// How a phase is cut.  The tile: 32 rows whose keys four waves share, if no owner has more, else 128.  Splits: while the tiles
+// of the batch do not fill the chip (two work-groups of 128 rows a compute unit), keys are split so that they do, in
+// stretches that pay for their partial results.
+static void shape_phase(const PhaseSums& s, int Hkv, int tile, AttendPhase* ph) {
+  ph->tile = tile;
+  const int64_t base = s.tiles * Hkv;
+  double chunk = (double)s.max_keys + 64;
+  if (base > 0 && base < 512) chunk = std::max(s.keys * Hkv / 512, tile == 128 ? 512.0 : 256.0);
+  chunk = std::max(chunk, s.max_keys / 64.0);
+  ph->chunk = (int32_t)std::min<int64_t>(((int64_t)chunk + 127) / 128 * 128, int64_t(1) << 30);
+  ph->splits = (int32_t)std::max<int64_t>(1, ceil_div(s.max_keys + 63, ph->chunk));  // (a tile's keys start at a multiple of 64)
+}
+
+static int plan_attend(const absb_layer* layer, const absb_batch* batch, const absb_rows* rows, const absb_shared_prefix* shared,
+                       const absb_score_opts* opts, AttendPlan* plan) {
+  int rc = check_dense_layer(layer);
+  if (rc != ABSB_OK) return rc;
+  if (!batch || !rows || !batch->seq_lens_host || !rows->row_off_host) return ABSB_ERR_NULL;
+  if (shared && (!shared->first_host || !shared->len_host)) return ABSB_ERR_NULL;
+  const int Bt = batch->batch, Hkv = layer->num_kv_heads, G = layer->num_q_heads / Hkv, P = layer->page_size;
+  if (Bt < 1 || Bt > 65535) return ABSB_ERR_BAD_SHAPE;
+  const int32_t *off = rows->row_off_host, *lens = batch->seq_lens_host;
+  if (off[0] != 0) return ABSB_ERR_BAD_SHAPE;
+  int64_t max_len = 0, max_n = 0;
+  for (int b = 0; b < Bt; ++b) {
+    if (off[b + 1] < off[b] || off[b + 1] - off[b] > lens[b]) return ABSB_ERR_BAD_SHAPE;
+    max_len = std::max<int64_t>(max_len, lens[b]);
+    max_n = std::max<int64_t>(max_n, off[b + 1] - off[b]);
+  }
+  if ((int64_t)batch->pt_stride < ceil_div(max_len, P)) return ABSB_ERR_BAD_SHAPE;
+  AttendPlan p = {};
+  p.rows = off[Bt];
+  PhaseSums own, common;
+  const int own_tile = max_n * G <= 32 ? 32 : 128;
+  int shared_tile = 32;
+  if (shared) {
+    const int32_t* first = shared->first_host;
+    if (shared->groups < 1 || first[0] != 0 || first[shared->groups] != Bt) return ABSB_ERR_BAD_SHAPE;
+    int64_t most = 0;
+    for (int g = 0; g < shared->groups; ++g) {
+      if (first[g + 1] < first[g] || first[g + 1] > Bt) return ABSB_ERR_BAD_SHAPE;
+      const int32_t len = shared->len_host[g];
+      if (len < 0 || len % P) return ABSB_ERR_BAD_SHAPE;
+      for (int b = first[g]; b < first[g + 1]; ++b)
+        if (lens[b] - (off[b + 1] - off[b]) < len) return ABSB_ERR_BAD_SHAPE;
+      most = std::max<int64_t>(most, off[first[g + 1]] - off[first[g]]);
+    }
+    shared_tile = most * G <= 32 ? 32 : 128;
+    for (int g = 0; g < shared->groups; ++g) {
+      const int64_t tiles = ceil_div((int64_t)(off[first[g + 1]] - off[first[g]]) * G, shared_tile);
+      common.tiles += tiles;
+      common.keys += (double)tiles * shared->len_host[g];
+      if (tiles) common.max_keys = std::max<int64_t>(common.max_keys, shared->len_host[g]);
+    }
+    p.shared.owners = shared->groups;
+    p.shared.slots = (int64_t)off[Bt] * G / shared_tile + shared->groups;
+    shape_phase(common, Hkv, shared_tile, &p.shared);
+    if (common.max_keys == 0) p.shared = AttendPhase{};  // nobody shares anything
+  }
+  const bool bounded = opts && opts->window && !opts->prefix_lens;  // no tile sees more keys than its window
+  PhaseSums seen;
+  int g = 0;
+  for (int b = 0; b < Bt; ++b) {
+    while (shared && b >= shared->first_host[g + 1]) ++g;
+    const int64_t n = off[b + 1] - off[b], tiles = ceil_div(n * G, own_tile);
+    if (!n) continue;
+    const int64_t keys = lens[b] - (shared ? shared->len_host[g] : 0);
+    const int64_t most = bounded ? std::min<int64_t>(keys, (int64_t)opts->window + own_tile / G + 1) : keys;
+    const double mean = keys - 0.5 * n;
+    own.tiles += tiles;
+    own.keys += mean * tiles;
+    own.max_keys = std::max(own.max_keys, keys);
+    seen.keys += std::min(mean, (double)most) * tiles;
+    seen.max_keys = std::max(seen.max_keys, most);
+  }
+  p.own.owners = Bt;
+  p.own.slots = (int64_t)off[Bt] * G / own_tile + Bt;
+  shape_phase(own, Hkv, own_tile, &p.own);
+  if (bounded) {  // never more splits than without the window: the workspace does not depend on the options
+    const int32_t splits = p.own.splits;
+    seen.tiles = own.tiles;
+    shape_phase(seen, Hkv, own_tile, &p.own);
+    if (p.own.splits > splits) {
+      p.own.chunk = (int32_t)(ceil_div(ceil_div(seen.max_keys + 63, splits), 128) * 128);
+      p.own.splits = (int32_t)ceil_div(seen.max_keys + 63, p.own.chunk);
+    }
+  }
+  p.parts = p.shared.splits + p.own.splits;
+  for (const AttendPhase* ph : {&p.shared, &p.own})
+    if (ph->slots * Hkv * ph->splits >= (int64_t(1) << 31)) return ABSB_ERR_BAD_SHAPE;
+  const int64_t pairs = p.rows * layer->num_q_heads;
+  if (ceil_div(pairs, 4) >= (int64_t(1) << 31)) return ABSB_ERR_BAD_SHAPE;
+  if (p.parts > 1 && p.rows) {
+    p.ws_part_ml = align256((size_t)pairs * p.parts * ABSB_HEAD_DIM * 4);
+    p.ws_bytes = p.ws_part_ml + align256((size_t)pairs * p.parts * 2 * 4);
+  }
+  *plan = p;
+  return ABSB_OK;
+}
+
 static float resolve_scale(const absb_layer* layer) {
   return layer->sm_scale > 0.0f ? layer->sm_scale : 1.0f / std::sqrt((float)layer->head_dim);
 }
@@ -549,6 +675,201 @@ int absb_assign_block_sizes(int32_t n_samples, int32_t n_heads, int32_t n_cand, 
     block_size_out[h] = cand[chosen];
   }
   return ABSB_OK;
+}
+
+// ------------------------------------------------------------------ around the cache
+
+int absb_map_rows(const absb_layer* layer, const absb_batch* batch, const int32_t* lens_before, int32_t* page_table,
+                  const absb_page_ring* ring, int32_t max_rows, int32_t* row_off, int32_t* row_pos, int64_t* row_slot,
+                  void* stream) {
+  if (!layer || !batch) return ABSB_ERR_NULL;
+  const int P = layer->page_size;
+  if (!is_pow2(P) || P < 8 || P > 65536) return ABSB_ERR_BAD_SHAPE;
+  if (batch->batch < 1 || batch->batch > 65535 || batch->pt_stride < 0 || max_rows < 0) return ABSB_ERR_BAD_SHAPE;
+  if (!lens_before || !batch->seq_lens || !row_off || (!page_table && batch->pt_stride)) return ABSB_ERR_NULL;
+  if (max_rows && (!row_pos || !row_slot)) return ABSB_ERR_NULL;
+  if (ring) {
+    if (ring->capacity < 1) return ABSB_ERR_BAD_SHAPE;
+    if (!ring->pages || !ring->cursors || !ring->cursors_out) return ABSB_ERR_NULL;
+  }
+  MapParams p = {};
+  p.before = lens_before;
+  p.after = batch->seq_lens;
+  p.page_table = page_table;
+  if (ring) {
+    p.ring = ring->pages;
+    p.cursors = ring->cursors;
+    p.cursors_out = ring->cursors_out;
+    p.capacity = ring->capacity;
+  }
+  p.row_off = row_off;
+  p.row_pos = row_pos;
+  p.row_slot = row_slot;
+  p.batch = batch->batch;
+  p.pt_stride = batch->pt_stride;
+  p.max_rows = max_rows;
+  p.log2_page = ilog2(P);
+  return launch_map_rows(p, static_cast<hipStream_t>(stream));
+}
+
+static int check_rope(const absb_rope* rope) {
+  if (!rope) return ABSB_ERR_NULL;
+  if (rope->rot_dim < 2 || rope->rot_dim > ABSB_HEAD_DIM || rope->rot_dim % 2) return ABSB_ERR_BAD_SHAPE;
+  if (rope->layout != ABSB_ROPE_HALVES && rope->layout != ABSB_ROPE_PAIRS) return ABSB_ERR_UNSUPPORTED;
+  if (!std::isfinite(rope->amplitude)) return ABSB_ERR_BAD_SHAPE;
+  return ABSB_OK;
+}
+
+int absb_rope_frequencies(const absb_rope* rope, double* freq_host) {
+  const int rc = check_rope(rope);
+  if (rc != ABSB_OK) return rc;
+  if (!freq_host) return ABSB_ERR_NULL;
+  const int kind = rope->scaling, R = rope->rot_dim;
+  if (kind < ABSB_ROPE_PLAIN || kind > ABSB_ROPE_BY_TURNS) return ABSB_ERR_UNSUPPORTED;
+  if (!(rope->base > 1.0) || std::isinf(rope->base)) return ABSB_ERR_BAD_SHAPE;
+  const double factor = kind == ABSB_ROPE_PLAIN ? 1.0 : rope->factor;
+  if (!(factor >= 1.0) || std::isinf(factor)) return ABSB_ERR_BAD_SHAPE;
+  if (kind == ABSB_ROPE_BASE && R == 2) return ABSB_ERR_BAD_SHAPE;
+  if (kind == ABSB_ROPE_BY_TURNS &&
+      (!(rope->original_len > 0.0) || std::isinf(rope->original_len) || !(rope->low_turns >= 0.0) ||
+       !(rope->high_turns > rope->low_turns) || std::isinf(rope->high_turns)))
+    return ABSB_ERR_BAD_SHAPE;
+  const double base = kind == ABSB_ROPE_BASE ? rope->base * std::pow(factor, (double)R / (R - 2)) : rope->base;
+  for (int i = 0; i < R / 2; ++i) {
+    double f = std::pow(base, -2.0 * i / R);
+    if (kind == ABSB_ROPE_LINEAR) f /= factor;
+    if (kind == ABSB_ROPE_BY_TURNS) {
+      const double turns = rope->original_len * f / 6.283185307179586;
+      const double keep = std::min(1.0, std::max(0.0, (turns - rope->low_turns) / (rope->high_turns - rope->low_turns)));
+      f = keep * f + (1.0 - keep) * f / factor;
+    }
+    freq_host[i] = f;
+  }
+  return ABSB_OK;
+}
+
+int absb_rotate_store(const absb_layer* layer, const absb_rope* rope, int32_t n_rows, const int32_t* row_pos,
+                      const int64_t* row_slot, const double* freq, const void* q, int64_t q_stride, void* q_out,
+                      const void* k, int64_t k_stride, const void* v, int64_t v_stride, void* k_cache, void* v_cache,
+                      void* stream) {
+  int rc = check_dense_layer(layer);
+  if (rc != ABSB_OK) return rc;
+  rc = check_rope(rope);
+  if (rc != ABSB_OK) return rc;
+  if (n_rows < 0) return ABSB_ERR_BAD_SHAPE;
+  if (n_rows == 0) return ABSB_OK;
+  if (!row_pos || !freq || !q != !q_out || !k != !v || (!q && !k)) return ABSB_ERR_NULL;
+  if (k && (!row_slot || !k_cache || !v_cache)) return ABSB_ERR_NULL;
+  const int Hq = layer->num_q_heads, Hkv = layer->num_kv_heads;
+  const int64_t dq = (int64_t)Hq * ABSB_HEAD_DIM, dk = (int64_t)Hkv * ABSB_HEAD_DIM;
+  if (q && (q_stride < dq || q_stride % 8 || (q == q_out && q_stride != dq))) return ABSB_ERR_BAD_SHAPE;
+  if (k && (k_stride < dk || k_stride % 8 || v_stride < dk || v_stride % 8)) return ABSB_ERR_BAD_SHAPE;
+  for (const void* at : {q, (const void*)q_out, k, v, (const void*)k_cache, (const void*)v_cache})
+    if (reinterpret_cast<uintptr_t>(at) & 15) return ABSB_ERR_BAD_SHAPE;
+  RotateParams p = {};
+  p.q = static_cast<const uint16_t*>(q);
+  p.k = static_cast<const uint16_t*>(k);
+  p.v = static_cast<const uint16_t*>(v);
+  p.q_out = static_cast<uint16_t*>(q_out);
+  p.k_cache = static_cast<uint16_t*>(k_cache);
+  p.v_cache = static_cast<uint16_t*>(v_cache);
+  p.q_stride = q_stride;
+  p.k_stride = k_stride;
+  p.v_stride = v_stride;
+  p.s_page = layer->kv_stride_page;
+  p.s_head = layer->kv_stride_head;
+  p.s_tok = layer->kv_stride_tok;
+  p.pos = row_pos;
+  p.slot = k ? row_slot : nullptr;
+  p.freq = freq;
+  p.amplitude = rope->amplitude != 0.0f ? rope->amplitude : 1.0f;
+  p.n_rows = n_rows;
+  p.nq = q ? Hq : 0;
+  p.nkv = k ? Hkv : 0;
+  p.rot = rope->rot_dim;
+  p.halves = rope->layout == ABSB_ROPE_HALVES;
+  p.log2_page = ilog2(layer->page_size);
+  return launch_rotate(p, layer->dtype, static_cast<hipStream_t>(stream));
+}
+
+int absb_attend_workspace(const absb_layer* layer, const absb_batch* batch, const absb_rows* rows,
+                          const absb_shared_prefix* shared, size_t* workspace_bytes) {
+  AttendPlan p;
+  int rc = plan_attend(layer, batch, rows, shared, nullptr, &p);
+  if (rc != ABSB_OK) return rc;
+  if (!workspace_bytes) return ABSB_ERR_NULL;
+  *workspace_bytes = p.ws_bytes;
+  return ABSB_OK;
+}
+
+static int attend(const absb_layer* layer, const absb_batch* batch, const absb_rows* rows, const absb_shared_prefix* shared,
+                  const void* q, const void* k_cache, const void* v_cache, void* out, float* lse,
+                  const absb_score_opts* opts, void* workspace, size_t workspace_bytes, void* stream) {
+  AttendPlan plan;
+  int rc = plan_attend(layer, batch, rows, shared, opts, &plan);
+  if (rc != ABSB_OK) return rc;
+  const float cap = opts ? opts->softcap : 0.0f;
+  if (!(cap >= 0.0f) || std::isinf(cap) || (opts && opts->window < 0)) return ABSB_ERR_BAD_SHAPE;
+  if (plan.rows == 0) return ABSB_OK;
+  if (!q || !k_cache || !v_cache || !out || !batch->seq_lens || !batch->page_table || !rows->row_off) return ABSB_ERR_NULL;
+  if (shared && (!shared->first || !shared->len)) return ABSB_ERR_NULL;
+  for (const void* at : {q, (const void*)out, k_cache, v_cache})
+    if (reinterpret_cast<uintptr_t>(at) & 15) return ABSB_ERR_BAD_SHAPE;
+  rc = check_ws(workspace, workspace_bytes, plan.ws_bytes);
+  if (rc != ABSB_OK) return rc;
+  AttendParams p = {};
+  p.q = static_cast<const uint16_t*>(q);
+  p.k = static_cast<const char*>(k_cache);
+  p.v = static_cast<const char*>(v_cache);
+  p.page_table = batch->page_table;
+  p.seq_lens = batch->seq_lens;
+  p.row_off = rows->row_off;
+  p.batch = batch->batch;
+  if (plan.shared.owners) {
+    p.first = shared->first;
+    p.len = shared->len;
+    p.groups = shared->groups;
+  }
+  if (opts) {
+    p.prefix_lens = opts->prefix_lens;
+    p.doc_start = opts->doc_start;
+    p.slopes = opts->slopes;
+    p.window = opts->window;
+  }
+  p.out = static_cast<uint16_t*>(out);
+  p.lse = lse;
+  p.part_o = static_cast<float*>(workspace);
+  p.part_ml = reinterpret_cast<float*>(static_cast<char*>(workspace) + plan.ws_part_ml);
+  p.s_page = layer->kv_stride_page * 2;
+  p.s_head = layer->kv_stride_head * 2;
+  p.s_tok = layer->kv_stride_tok * 2;
+  p.pt_stride = batch->pt_stride;
+  p.Hq = layer->num_q_heads;
+  p.Hkv = layer->num_kv_heads;
+  p.G = p.Hq / p.Hkv;
+  p.log2_page = ilog2(layer->page_size);
+  p.parts = plan.parts;
+  const float scale = resolve_scale(layer);
+  p.scale_log2 = scale * 1.4426950408889634f;
+  if (cap > 0.0f) {
+    p.cap_log2 = cap * 1.4426950408889634f;
+    p.cap_in = scale / cap;
+    p.cap_wide = cap > 256.0f;
+  }
+  return launch_attend(p, plan, layer->dtype, cap > 0.0f, static_cast<hipStream_t>(stream));
+}
+
+int absb_attend_rows(const absb_layer* layer, const absb_batch* batch, const absb_rows* rows, const void* q,
+                     const void* k_cache, const void* v_cache, void* out, float* lse, const absb_score_opts* opts,
+                     void* workspace, size_t workspace_bytes, void* stream) {
+  return attend(layer, batch, rows, nullptr, q, k_cache, v_cache, out, lse, opts, workspace, workspace_bytes, stream);
+}
+
+int absb_attend_shared(const absb_layer* layer, const absb_batch* batch, const absb_rows* rows,
+                       const absb_shared_prefix* shared, const void* q, const void* k_cache, const void* v_cache, void* out,
+                       float* lse, const absb_score_opts* opts, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!shared) return ABSB_ERR_NULL;
+  return attend(layer, batch, rows, shared, q, k_cache, v_cache, out, lse, opts, workspace, workspace_bytes, stream);
 }
 
 int absb_stream_read(const void* src, size_t bytes, void* sink, void* stream) {

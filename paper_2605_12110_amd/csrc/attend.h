@@ -1,0 +1,48 @@
+// Dense attention of new rows over the paged cache: what the host plans and the kernels in attend.hip take.
+#pragma once
+#include "common.h"
+
+namespace absb {
+
+// A phase of a call: the rows of "owners" against the keys that an owner holds.  Own keys: an owner is a request.  Shared keys: an
+// owner is a group of requests, its keys the group's prefix.  An owner's rows, n tokens of G query heads a KV head, are cut
+// into tiles; owner o's tiles are slots floor(row_off[o] * G / tile) + o and on, which leaves room for all of them
+// and can be searched without a list; a slot without rows leaves at once.
+struct AttendPhase {
+  int32_t owners;
+  int32_t tile;    // rows (token, query head of the group) of a work-group: 128, or 32 that its four waves share
+  int32_t splits;  // of a tile's keys, a work-group each
+  int32_t chunk;   // keys of a split, a multiple of 128
+  int64_t slots;   // tiles, empty ones included
+};
+
+struct AttendPlan {
+  AttendPhase shared, own;  // shared.owners = 0: no such phase
+  int32_t parts;            // partial results of a row: shared.splits + own.splits
+  int64_t rows;
+  size_t ws_part_ml, ws_bytes;  // ws_bytes = 0: one part, written straight to the output
+};
+
+struct AttendParams {
+  const uint16_t* q;
+  const char *k, *v;
+  const int32_t *page_table, *seq_lens, *row_off;
+  const int32_t *first, *len;  // groups: first request, shared tokens (null: none)
+  const int32_t *prefix_lens, *doc_start;
+  const float* slopes;
+  uint16_t* out;
+  float* lse;
+  float* part_o;   // [rows][Hq][parts][128], not normalised
+  float* part_ml;  // [rows][Hq][parts][2]: maximum in log2 units, sum
+  int64_t s_page, s_head, s_tok;  // bytes
+  int32_t batch, groups, pt_stride, Hq, Hkv, G, log2_page;
+  int32_t window, parts, part0;   // part0: of this phase's first split
+  float scale_log2;               // sm_scale * log2(e)
+  float cap_log2, cap_in;         // cap * log2(e), sm_scale / cap (capped only)
+  int32_t cap_wide;               // 1: the cap is so far above ordinary scores that small ones need the series
+  AttendPhase phase;
+};
+
+ABSB_HIDDEN int launch_attend(const AttendParams& p, const AttendPlan& plan, int dtype, bool capped, hipStream_t stream);
+
+}  // namespace absb

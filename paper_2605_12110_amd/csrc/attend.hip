@@ -1,0 +1,505 @@
+// Dense attention of new rows over the paged cache (absb_attend_rows, absb_attend_shared).
+//
+// Every row sees an interval of keys: causal order, window, documents, prefixes and shared prefixes all bound it from below or
+// above.  A tile of rows (token, query head of one KV head's group) goes over the keys of its rows' intervals block by block with
+// the running maximum and sum of a softmax; blocks that all rows see need no mask, blocks that none sees are not read.
+//
+//   S^T = K Q^T  32 keys x 32 rows in a 32x32x16 product: a lane then holds 16 scores of ONE row (row = lane % 32), so
+//                maxima and sums are a lane's own but for one exchange with lane ^ 32, and a row's factors need no
+//                broadcast;
+//   O^T += V^T P^T  32 channels x 32 rows: with the keys taken in the order in which the lanes hold them, S^T's registers,
+//                rounded in pairs, are the operand P^T as they stand.  V^T comes from row-major V by the transposing read.
+//
+// K and V are copied from their pages straight to LDS, a block ahead, 16 bytes a lane.  The copy writes lanes side by side, so
+// what spreads a read over the banks is which piece of a row a lane fetches: K's piece p of row r lies at p ^ (r % 16), V's at
+// p ^ 4 (r % 4).
+#include "attend.h"
+
+namespace absb {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int ATT_THREADS = 256, ATT_WAVES = 4;
+constexpr int ROW_BYTES = ABSB_HEAD_DIM * 2;
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+template <int DT>
+__device__ __forceinline__ f32x16 mma_32x32x16(u32x4 a, u32x4 b, f32x16 c) {
+  if (DT == ABSB_F16)
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(bitcast<half8_t>(a), bitcast<half8_t>(b), c, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(bitcast<bf16x8_t>(a), bitcast<bf16x8_t>(b), c, 0, 0, 0);
+}
+
+// Two values rounded to the K/V type, side by side.
+template <int DT>
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  if (DT == ABSB_F16) {
+    half2_t h = {(_Float16)a, (_Float16)b};
+    return bitcast<uint32_t>(h);
+  }
+  bf16x2_t h = {(__bf16)a, (__bf16)b};
+  return bitcast<uint32_t>(h);
+}
+
+// The other half of the wave's value.
+template <typename Op>
+__device__ __forceinline__ float across_halves(float x, Op op) {
+  const auto h = __builtin_amdgcn_permlane32_swap(bitcast<uint32_t>(x), bitcast<uint32_t>(x), false, false);
+  return op(bitcast<float>(h[0]), bitcast<float>(h[1]));
+}
+
+// Largest o in [0, n) with slot0(o) <= x, slot0 increasing, slot0(0) <= x; the wave looks at 64 places at a time.
+template <typename F>
+__device__ __forceinline__ int last_at_most(int n, int64_t x, F slot0) {
+  int lo = 0, hi = n;
+  const int lane = threadIdx.x & 63;
+  while (hi - lo > 1) {
+    const int step = (hi - lo + 63) >> 6, at = lo + lane * step;
+    const uint64_t below = __ballot(at < hi && slot0(min(at, hi - 1)) <= x);
+    lo += (__popcll(below) - 1) * step;
+    hi = min(hi, lo + step);
+  }
+  return lo;
+}
+
+struct RowOf {
+  int row, head;       // row of q and out, query head; row < 0: none
+  int pos, lo, hi;     // position, first and last key seen
+};
+
+// What a work-group's tile is about.
+struct Tile {
+  int table_row, limit;     // whose page-table row; keys it holds
+  int r0, n;                // first row, rows (tokens)
+  int64_t f0;               // first (token, head) pair of the tile
+};
+
+// Softmax state and output of a wave's 32 rows: lane l holds row l % 32; O[t][i] is channel 32 t + 8 (i / 4) + 4 (l / 32) + i % 4.
+struct State {
+  float m, l;
+  f32x16 o[4];
+};
+
+// Scores in log2 units, from S = q.k: the cap, then the distance bias.
+template <bool CAP, bool BIAS>
+__device__ __forceinline__ float score_of(const AttendParams& p, float s, float slope_log2, int pos, int key) {
+  float x;
+  if (CAP) {
+    // cap tanh(y) = cap - 2 cap / (e^2y + 1), off by 2^-23 cap; where that is too much, small y by the series
+    const float y = s * p.cap_in, t = exp2_fast(y * (2.0f * LOG2E));
+    x = __builtin_fmaf(-2.0f * p.cap_log2, __builtin_amdgcn_rcpf(t + 1.0f), p.cap_log2);
+    if (p.cap_wide) {
+      const float z = y * y;
+      const float series = y * (1.0f + z * (-1.0f / 3 + z * (2.0f / 15 + z * (-17.0f / 315 + z * (62.0f / 2835)))));
+      x = __builtin_fabsf(y) < 0.25f ? series * p.cap_log2 : x;
+    }
+  } else {
+    x = s * p.scale_log2;
+  }
+  if (BIAS) x -= slope_log2 * (float)__builtin_abs(pos - key);
+  return x;
+}
+
+// 32 KT keys in LDS (K's rows at `kl`, V's at `vl`) folded into the state.  `k0`: the first one's index; MASK: some row of
+// the wave does not see all of them.
+template <int DT, bool CAP, bool BIAS, int KT>
+__device__ __forceinline__ void fold_keys(const AttendParams& p, const char* kl, const char* vl, int k0, bool mask, const u32x4 (&q)[8],
+                                          const RowOf& row, float slope_log2, State& st) {
+  const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
+  f32x16 s[KT];
+#pragma unroll
+  for (int t = 0; t < KT; ++t) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      const u32x4 a = *reinterpret_cast<const u32x4*>(kl + (32 * t + col) * ROW_BYTES + (((2 * c + half) ^ (col & 15)) * 16));
+      s[t] = mma_32x32x16<DT>(a, q[c], s[t]);
+    }
+  }
+  float mx = -__builtin_inff();
+#pragma unroll
+  for (int t = 0; t < KT; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int key = k0 + 32 * t + 8 * (i >> 2) + 4 * half + (i & 3);
+      float x = (CAP || BIAS) ? score_of<CAP, BIAS>(p, s[t][i], slope_log2, row.pos, key) : s[t][i];
+      if (mask) x = key >= row.lo && key <= row.hi ? x : -__builtin_inff();
+      s[t][i] = x;
+      mx = fmaxf(mx, x);
+    }
+  mx = across_halves(mx, [](float a, float b) { return fmaxf(a, b); });
+  constexpr bool SCALED = CAP || BIAS;  // (else the scores are still q.k)
+  const float mn = fmaxf(st.m, SCALED ? mx : mx * p.scale_log2);
+  const float base = mn == -__builtin_inff() ? 0.0f : mn;  // nothing seen yet: weights 0, not NaN
+  const float alpha = exp2_fast(st.m - base);
+  st.m = mn;
+  float sum = 0.0f;
+#pragma unroll
+  for (int t = 0; t < KT; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s[t][i] = exp2_fast(SCALED ? s[t][i] - base : __builtin_fmaf(s[t][i], p.scale_log2, -base));
+      sum += s[t][i];
+    }
+  st.l = __builtin_fmaf(st.l, alpha, sum);
+  if (__any(alpha != 1.0f)) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) st.o[t] *= alpha;
+  }
+#pragma unroll
+  for (int c = 0; c < 2 * KT; ++c) {
+    u32x4 w;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = pack2<DT>(s[c >> 1][8 * (c & 1) + 2 * j], s[c >> 1][8 * (c & 1) + 2 * j + 1]);
+    // V^T: of 16 lanes, lane i points at channels 4 (i % 4).. of key i / 4 and gets channel i of the four keys
+    const int i16 = lane & 15, grp = (lane >> 4) & 1, key = 16 * c + 4 * half + (i16 >> 2);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int piece = (4 * t + 2 * grp + ((i16 & 3) >> 1)) ^ ((key & 3) << 2);
+      const char* at = vl + key * ROW_BYTES + piece * 16 + (i16 & 1) * 8;
+      typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
+      const u32x2 lo = bitcast<u32x2>(__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(at)));
+      const u32x2 hi = bitcast<u32x2>(__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(at + 8 * ROW_BYTES)));
+      st.o[t] = mma_32x32x16<DT>(u32x4{lo[0], lo[1], hi[0], hi[1]}, w, st.o[t]);
+    }
+  }
+}
+
+__device__ __forceinline__ uint64_t lane_u64(uint64_t v, int lane) {
+  return (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane) |
+         ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), lane) << 32);
+}
+
+// Where the rows of 512 keys lie: lane j of the wave has the byte offset of keys 8 j .. 8 j + 7 of the stretch (they share a
+// page) and which of the eight is the last that exists.
+struct Stretch {
+  uint64_t off;
+  int most;
+};
+__device__ __forceinline__ Stretch look_up(const AttendParams& p, const int32_t* pages, int k0, int limit) {
+  const int lane = threadIdx.x & 63;
+  const int key = min((int64_t)k0 + 8 * lane, (int64_t)limit - 1), at = key & ~7;
+  Stretch s;
+  s.off = (uint64_t)pages[at >> p.log2_page] * (uint64_t)p.s_page +
+          (uint64_t)(at & ((1 << p.log2_page) - 1)) * (uint64_t)p.s_tok;
+  s.most = min(7, limit - 1 - at);
+  return s;
+}
+
+// Copies rows 4 i .. 4 i + 3 of the wave's rows of a block to LDS: eight keys' offset and last row from lane `from` of the
+// stretch, the upper four of them if `upper`.
+__device__ __forceinline__ void copy_rows(const AttendParams& p, const char* k, const char* v, const Stretch& s, int from, int i,
+                                          char* kl, char* vl) {
+  const int lane = threadIdx.x & 63, piece = lane & 15, r4 = lane >> 4;
+  const uint64_t off = lane_u64(s.off, from);
+  const int most = __builtin_amdgcn_readlane(s.most, from);
+  const uint64_t row = off + (uint64_t)min(4 * (i & 1) + r4, most) * (uint64_t)p.s_tok;
+  typedef __attribute__((address_space(1))) const void* gptr;
+  typedef __attribute__((address_space(3))) void* lptr;
+  __builtin_amdgcn_global_load_lds((gptr)(k + row + ((piece ^ (4 * (i & 3) + r4)) * 16)), (lptr)(kl + 4 * i * ROW_BYTES), 16, 0, 0);
+  __builtin_amdgcn_global_load_lds((gptr)(v + row + ((piece ^ (r4 << 2)) * 16)), (lptr)(vl + 4 * i * ROW_BYTES), 16, 0, 0);
+}
+
+// The wave's copies have arrived, and what it read of LDS has, too (the next copy may overwrite it).
+__device__ __forceinline__ void copies_done() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
+
+// The interval of a row, and the row itself: pair f = f0 + i of the tile.
+template <bool SHARED>
+__device__ __forceinline__ RowOf row_of(const AttendParams& p, const Tile& t, int own_from, int group, int kv_head, int64_t f) {
+  RowOf r;
+  r.row = -1;
+  r.head = kv_head * p.G;
+  r.pos = 0;
+  r.lo = 0;
+  r.hi = -1;
+  if (f >= (int64_t)t.n * p.G) return r;
+  const int tok = (int)((uint64_t)f / (uint32_t)p.G), g = (int)(f - (int64_t)tok * p.G);
+  r.row = t.r0 + tok;
+  r.head += g;
+  int b = t.table_row;
+  if (SHARED) {
+    r.hi = t.limit - 1;
+    if (p.window || p.slopes) {  // the request that the row belongs to
+      int lo = p.first[group], hi = p.first[group + 1];
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (p.row_off[mid] <= r.row) lo = mid; else hi = mid;
+      }
+      r.pos = p.seq_lens[lo] - (p.row_off[lo + 1] - r.row);
+    }
+  } else {
+    r.pos = t.limit - t.n + tok;
+    r.hi = r.pos;
+    if (p.prefix_lens) r.hi = min(max(r.hi, p.prefix_lens[b] - 1), t.limit - 1);
+    r.lo = own_from;
+  }
+  if (p.window) r.lo = max(r.lo, r.pos - p.window + 1);
+  if (p.doc_start) r.lo = max(r.lo, p.doc_start[r.row]);
+  return r;
+}
+
+template <int DT, bool CAP, bool BIAS, bool SHARED, bool WIDE>
+__global__ __launch_bounds__(ATT_THREADS, WIDE ? 2 : 1) void attend_kernel(AttendParams p) {
+  constexpr int TILE = WIDE ? 128 : 32;
+  // WIDE: a block of 64 keys that all waves use, twice.  Otherwise: 32 keys a wave, twice, and later the waves' outputs.
+  constexpr int STAGE = WIDE ? 64 * ROW_BYTES : 32 * ROW_BYTES;  // of K, and of V
+  __shared__ __align__(16) char s_kv[WIDE ? 4 * STAGE : 4 * STAGE * ATT_WAVES];
+  __shared__ int s_lo[ATT_WAVES], s_hi[ATT_WAVES];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+
+  // ---- which tile, KV head and split: heads go round the dies first, so that a head's keys stay in one die's L2 where there
+  // are eight; long tiles (the last of a causal prompt) start first
+  const uint32_t unit = blockIdx.x;
+  const int kv_head = (int)(unit % (uint32_t)p.Hkv);
+  const uint32_t rest = unit / (uint32_t)p.Hkv;
+  const int split = (int)(rest % (uint32_t)p.phase.splits);
+  const int64_t slot = p.phase.slots - 1 - (int64_t)(rest / (uint32_t)p.phase.splits);
+  auto row0 = [&](int o) { return p.row_off[SHARED ? p.first[o] : o]; };
+  auto slot0 = [&](int o) { return (int64_t)row0(o) * p.G / TILE + o; };
+  const int owner = last_at_most(p.phase.owners, slot, slot0);
+  Tile t;
+  t.r0 = row0(owner);
+  t.n = row0(owner + 1) - t.r0;
+  t.f0 = (slot - slot0(owner)) * TILE;
+  if (t.f0 >= (int64_t)t.n * p.G) return;
+  t.table_row = SHARED ? p.first[owner] : owner;
+  t.limit = SHARED ? p.len[owner] : p.seq_lens[owner];
+  int own_from = 0;
+  if (!SHARED && p.first) own_from = p.len[last_at_most(p.groups, owner, [&](int g) { return (int64_t)p.first[g]; })];
+
+  const RowOf row = row_of<SHARED>(p, t, own_from, owner, kv_head, t.f0 + (WIDE ? 32 * wave : 0) + (lane & 31));
+  const bool valid = row.row >= 0, sees = valid && row.lo <= row.hi;
+  const int lo = sees ? row.lo : INT32_MAX, hi = sees ? row.hi : -1;
+  auto lesser = [](uint32_t a, uint32_t b) { return a < b ? a : b; };
+  auto greater = [](uint32_t a, uint32_t b) { return a > b ? a : b; };
+  const int wave_lo = (int)wave_reduce_u32((uint32_t)lo, lesser), wave_hi = (int)wave_reduce_u32((uint32_t)(hi + 1), greater) - 1;
+  // keys that every row of the wave sees (rows that do not exist see whatever the others do)
+  const int all_lo = (int)wave_reduce_u32((uint32_t)(valid ? row.lo : 0), greater);
+  const int all_hi = (int)wave_reduce_u32((uint32_t)((valid ? row.hi : INT32_MAX - 1) + 1), lesser) - 1;
+  int tile_lo = wave_lo, tile_hi = wave_hi;
+  if (WIDE) {
+    if (lane == 0) {
+      s_lo[wave] = wave_lo;
+      s_hi[wave] = wave_hi;
+    }
+    __syncthreads();
+    tile_lo = min(min(s_lo[0], s_lo[1]), min(s_lo[2], s_lo[3]));
+    tile_hi = max(max(s_hi[0], s_hi[1]), max(s_hi[2], s_hi[3]));
+  }
+  State st;
+  st.m = -__builtin_inff();
+  st.l = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) st.o[i][j] = 0.0f;
+
+  // ---- the split's keys [begin, end)
+  const int64_t from = ((int64_t)tile_lo & ~int64_t(63)) + (int64_t)split * p.phase.chunk;
+  const int begin = (int)min(from, (int64_t)tile_hi + 1);
+  const int end = (int)min(from + p.phase.chunk, (int64_t)tile_hi + 1);
+  if (begin < end) {
+    u32x4 q[8];
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      q[c] = u32x4{0u, 0u, 0u, 0u};
+      if (valid) q[c] = *reinterpret_cast<const u32x4*>(p.q + ((int64_t)row.row * p.Hq + row.head) * ABSB_HEAD_DIM + (2 * c + (lane >> 5)) * 8);
+    }
+    const float slope_log2 = BIAS && valid ? p.slopes[row.head] * LOG2E : 0.0f;
+    const int32_t* pages = p.page_table + (int64_t)t.table_row * p.pt_stride;
+    const char *kb = p.k + kv_head * p.s_head, *vb = p.v + kv_head * p.s_head;
+    // Stretches of 512 keys from `begin` on; a step is 64 keys (WIDE), or 128, 32 a wave.
+    constexpr int STEP = WIDE ? 64 : 128;
+    const int steps = (end - begin + STEP - 1) / STEP;
+    Stretch now = look_up(p, pages, begin, t.limit), next = now;
+    char* mine = WIDE ? s_kv : s_kv + wave * 4 * STAGE;
+    auto copy = [&](int i, int buf) __attribute__((always_inline)) {
+      char *kl = mine + buf * 2 * STAGE, *vl = kl + STAGE;
+      const Stretch& s = now;
+      if (WIDE) {
+        kl += 16 * wave * ROW_BYTES;
+        vl += 16 * wave * ROW_BYTES;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) copy_rows(p, kb, vb, s, (i & 7) * 8 + 2 * wave + (j >> 1), j, kl, vl);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) copy_rows(p, kb, vb, s, (i & 3) * 16 + 4 * wave + (j >> 1), j, kl, vl);
+      }
+    };
+    constexpr int PER = 512 / STEP;  // steps of a stretch
+    copy(0, 0);
+    for (int i = 0; i < steps; ++i) {
+      copies_done();
+      if (WIDE) __syncthreads();  // ... everybody's, and nobody reads the other buffer any more
+      if (i + 1 < steps) {
+        if ((i + 1) % PER == 0) now = next;
+        copy(i + 1, (i + 1) & 1);
+        if ((i + 1) % PER == 0 || i == 0) next = look_up(p, pages, (int)min((int64_t)begin + ((i + 1) / PER + 1) * 512, (int64_t)t.limit - 1), t.limit);
+      }
+      const int k0 = begin + i * STEP + (WIDE ? 0 : 32 * wave), k1 = k0 + (WIDE ? 63 : 31);
+      const char* kl = mine + (i & 1) * 2 * STAGE;
+      if (k0 > wave_hi || k1 < wave_lo) continue;
+      // a split ends on a block or with the tile's last key, so what a row sees of a block is in its interval
+      const bool mask = k0 < all_lo || k1 > all_hi;
+      fold_keys<DT, CAP, BIAS, WIDE ? 2 : 1>(p, kl, kl + STAGE, k0, mask, q, row, slope_log2, st);
+    }
+  }
+  st.l = across_halves(st.l, [](float a, float b) { return a + b; });
+
+  // ---- the waves of a narrow tile have keys of their own: their states become one, wave w's quarter of the channels of all
+  if (!WIDE) {
+    __syncthreads();
+    float* s_o = reinterpret_cast<float*>(s_kv);             // [wave][channel][row], 16 KB a wave
+    float* s_ml = reinterpret_cast<float*>(s_kv + 65536);    // [wave][2][32]
+    const int half = lane >> 5, col = lane & 31;
+    if (half == 0) {
+      s_ml[wave * 64 + col] = st.m;
+      s_ml[wave * 64 + 32 + col] = st.l;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) s_o[wave * 4096 + (32 * i + 8 * (j >> 2) + 4 * half + (j & 3)) * 32 + col] = st.o[i][j];
+    __syncthreads();
+    float m = -__builtin_inff(), w[ATT_WAVES];
+#pragma unroll
+    for (int x = 0; x < ATT_WAVES; ++x) m = fmaxf(m, s_ml[x * 64 + col]);
+    const float base = m == -__builtin_inff() ? 0.0f : m;
+    float l = 0.0f;
+#pragma unroll
+    for (int x = 0; x < ATT_WAVES; ++x) {
+      w[x] = exp2_fast(s_ml[x * 64 + col] - base);
+      l = __builtin_fmaf(s_ml[x * 64 + 32 + col], w[x], l);
+    }
+    st.m = m;
+    st.l = l;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      const int at = (32 * wave + 8 * (j >> 2) + 4 * half + (j & 3)) * 32 + col;
+      float v = 0.0f;
+#pragma unroll
+      for (int x = 0; x < ATT_WAVES; ++x) v = __builtin_fmaf(s_o[x * 4096 + at], w[x], v);
+      st.o[0][j] = v;
+    }
+  }
+  if (!valid) return;
+
+  // ---- out: channels 32 t + 8 (i / 4) + 4 half + i % 4, four at a time
+  const int half = lane >> 5;
+  const int64_t at = (int64_t)row.row * p.Hq + row.head;
+  const bool writes_ml = half == 0 && (WIDE || wave == 0);
+  constexpr int TILES = WIDE ? 4 : 1;
+  if (p.parts == 1) {
+    const float inv = st.l > 0.0f ? 1.0f / st.l : 0.0f;
+#pragma unroll
+    for (int i = 0; i < TILES; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int ch = 32 * (WIDE ? i : wave) + 8 * j + 4 * half;
+        const uint2 w = {pack2<DT>(st.o[i][4 * j] * inv, st.o[i][4 * j + 1] * inv), pack2<DT>(st.o[i][4 * j + 2] * inv, st.o[i][4 * j + 3] * inv)};
+        *reinterpret_cast<uint2*>(p.out + at * ABSB_HEAD_DIM + ch) = w;
+      }
+    if (writes_ml && p.lse) p.lse[at] = st.l > 0.0f ? (st.m + __builtin_log2f(st.l)) * LN2 : -__builtin_inff();
+    return;
+  }
+  const int64_t part = at * p.parts + p.part0 + split;
+  if (writes_ml) *reinterpret_cast<float2*>(p.part_ml + part * 2) = make_float2(st.m, st.l);
+  if (begin < end) {  // (a split without keys has weight 0: its sum says so)
+#pragma unroll
+    for (int i = 0; i < TILES; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int ch = 32 * (WIDE ? i : wave) + 8 * j + 4 * half;
+        *reinterpret_cast<f32x4*>(p.part_o + part * ABSB_HEAD_DIM + ch) = f32x4{st.o[i][4 * j], st.o[i][4 * j + 1], st.o[i][4 * j + 2], st.o[i][4 * j + 3]};
+      }
+  }
+}
+
+// The parts of a (row, query head), a wave each: a lane has two channels.
+template <int DT>
+__global__ __launch_bounds__(256) void attend_merge_kernel(AttendParams p, int64_t pairs) {
+  const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (at >= pairs) return;
+  const int lane = threadIdx.x & 63;
+  const float* ml = p.part_ml + at * p.parts * 2;
+  const float* o = p.part_o + at * p.parts * ABSB_HEAD_DIM + 2 * lane;
+  float M = -__builtin_inff(), L = 0.0f, x = 0.0f, y = 0.0f;
+  for (int i0 = 0; i0 < p.parts; i0 += 64) {
+    float2 mine = make_float2(-__builtin_inff(), 0.0f);
+    if (i0 + lane < p.parts) mine = *reinterpret_cast<const float2*>(ml + (i0 + lane) * 2);
+    if (!(mine.y > 0.0f)) mine.x = -__builtin_inff();
+    const float top = fmaxf(M, wave_max_f32(mine.x)), base = top == -__builtin_inff() ? 0.0f : top;
+    const float a = exp2_fast(M - base), w = exp2_fast(mine.x - base);
+    M = top;
+    L *= a;
+    x *= a;
+    y *= a;
+    const int n = min(64, p.parts - i0);
+    for (int i = 0; i < n; ++i) {
+      const float wi = bitcast<float>(__builtin_amdgcn_readlane(bitcast<int>(w), i));
+      if (wi == 0.0f) continue;  // (its output may never have been written)
+      const float li = bitcast<float>(__builtin_amdgcn_readlane(bitcast<int>(mine.y), i));
+      const float2 v = *reinterpret_cast<const float2*>(o + (int64_t)(i0 + i) * ABSB_HEAD_DIM);
+      L = __builtin_fmaf(li, wi, L);
+      x = __builtin_fmaf(v.x, wi, x);
+      y = __builtin_fmaf(v.y, wi, y);
+    }
+  }
+  const float inv = L > 0.0f ? 1.0f / L : 0.0f;
+  *reinterpret_cast<uint32_t*>(p.out + at * ABSB_HEAD_DIM + 2 * lane) = pack2<DT>(x * inv, y * inv);
+  if (p.lse && lane == 0) p.lse[at] = L > 0.0f ? (M + __builtin_log2f(L)) * LN2 : -__builtin_inff();
+}
+
+template <int DT, bool CAP, bool BIAS, bool SHARED>
+static void launch_tiles(const AttendParams& p, dim3 grid, hipStream_t stream) {
+  if (p.phase.tile == 128)
+    hipLaunchKernelGGL((attend_kernel<DT, CAP, BIAS, SHARED, true>), grid, dim3(ATT_THREADS), 0, stream, p);
+  else
+    hipLaunchKernelGGL((attend_kernel<DT, CAP, BIAS, SHARED, false>), grid, dim3(ATT_THREADS), 0, stream, p);
+}
+template <int DT, bool CAP, bool BIAS>
+static void launch_phases(AttendParams p, const AttendPlan& plan, hipStream_t stream) {
+  auto grid = [&](const AttendPhase& ph) { return dim3((unsigned)(ph.slots * p.Hkv * ph.splits)); };
+  if (plan.shared.owners) {
+    p.phase = plan.shared;
+    p.part0 = 0;
+    launch_tiles<DT, CAP, BIAS, true>(p, grid(p.phase), stream);
+  }
+  p.phase = plan.own;
+  p.part0 = plan.parts - plan.own.splits;
+  launch_tiles<DT, CAP, BIAS, false>(p, grid(p.phase), stream);
+  if (plan.parts > 1) {
+    const int64_t pairs = plan.rows * p.Hq;
+    hipLaunchKernelGGL((attend_merge_kernel<DT>), dim3((unsigned)((pairs + 3) / 4)), dim3(256), 0, stream, p, pairs);
+  }
+}
+template <int DT>
+static void launch_typed(const AttendParams& p, const AttendPlan& plan, bool capped, hipStream_t stream) {
+  if (capped && p.slopes)
+    launch_phases<DT, true, true>(p, plan, stream);
+  else if (capped)
+    launch_phases<DT, true, false>(p, plan, stream);
+  else if (p.slopes)
+    launch_phases<DT, false, true>(p, plan, stream);
+  else
+    launch_phases<DT, false, false>(p, plan, stream);
+}
+
+int launch_attend(const AttendParams& p, const AttendPlan& plan, int dtype, bool capped, hipStream_t stream) {
+  if (dtype == ABSB_F16)
+    launch_typed<ABSB_F16>(p, plan, capped, stream);
+  else
+    launch_typed<ABSB_BF16>(p, plan, capped, stream);
+  return check_launch();
+}
+
+}  // namespace absb

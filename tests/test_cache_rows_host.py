@@ -1,0 +1,225 @@
+"""Host side of the entry points around the cache (no GPU): frequencies of rotary positions against their formulas, workspace sizes,
+and what is refused before anything is enqueued.  Addresses here are never followed: every call is refused, or has
+nothing to do."""
+import ctypes as C
+import math
+import os
+
+import numpy as np
+import pytest
+
+from paper_2605_12110_amd import absb
+
+D, AT = 128, 1 << 20      # AT: a 16-byte aligned address that nobody follows
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    if not os.path.exists(absb.LIB_PATH):
+        from paper_2605_12110_amd.build import build_library
+        build_library(force=False)
+
+
+def _layer(**kw):
+    d = dict(num_q_heads=32, num_kv_heads=8, head_dim=D, page_size=64, dtype=absb.F16, block_size=None,
+             kv_strides=(8 * 64 * D, 64 * D, D))
+    d.update(kw)
+    return absb.Layer(**d)
+
+
+def _batch(lens, width=None, P=64):
+    return absb.Batch(seq_lens_host=list(lens), seq_lens=AT, page_table=AT, pt_stride=(max(lens) + P - 1) // P if width is None else width)
+
+
+def _rows(new):
+    return absb.Rows(np.concatenate([[0], np.cumsum(new)]).astype(np.int32), AT)
+
+
+def _refused(status, f, *a, **kw):
+    with pytest.raises(absb.AbsbError) as e:
+        f(*a, stream=0, **kw)
+    assert e.value.status == status, e.value
+
+
+# ------------------------------------------------------------------ frequencies
+@pytest.mark.parametrize("R", [2, 4, 64, 96, 126, 128])
+def test_frequencies_plain_linear_and_base(R):
+    i = np.arange(R // 2)
+    f = absb.absb_rope_frequencies(absb.Rope(rot_dim=R, base=500000.0))
+    assert np.allclose(f, 500000.0 ** (-2.0 * i / R), rtol=1e-14) and f[0] == 1.0
+    lin = absb.absb_rope_frequencies(absb.Rope(rot_dim=R, base=500000.0, scaling=absb.ROPE_LINEAR, factor=8.0))
+    assert np.allclose(lin, f / 8.0, rtol=1e-14)
+    if R > 2:      # the lowest frequency is divided by the factor, the highest stays
+        b = absb.absb_rope_frequencies(absb.Rope(rot_dim=R, base=500000.0, scaling=absb.ROPE_BASE, factor=8.0))
+        assert b[0] == 1.0 and math.isclose(b[-1], f[-1] / 8.0, rel_tol=1e-12) and (np.diff(b) < 0).all()
+
+
+def test_frequencies_by_turns():
+    rope = absb.Rope(rot_dim=128, base=500000.0, scaling=absb.ROPE_BY_TURNS, factor=8.0, original_len=8192.0, low_turns=1.0, high_turns=4.0)
+    f0, f = absb.absb_rope_frequencies(absb.Rope(base=500000.0)), absb.absb_rope_frequencies(rope)
+    turns = 8192.0 * f0 / (2 * math.pi)
+    assert (turns > 4).any() and (turns < 1).any() and ((turns > 1) & (turns < 4)).any()
+    for t, a, b in zip(turns, f0, f):
+        keep = min(1.0, max(0.0, (t - 1.0) / 3.0))
+        assert math.isclose(b, a * keep + a / 8.0 * (1 - keep), rel_tol=1e-13)
+    assert np.array_equal(f[turns >= 4], f0[turns >= 4])
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(rot_dim=0), absb.ERR_BAD_SHAPE), (dict(rot_dim=3), absb.ERR_BAD_SHAPE), (dict(rot_dim=130), absb.ERR_BAD_SHAPE),
+    (dict(layout=2), absb.ERR_UNSUPPORTED), (dict(scaling=4), absb.ERR_UNSUPPORTED), (dict(scaling=-1), absb.ERR_UNSUPPORTED),
+    (dict(base=1.0), absb.ERR_BAD_SHAPE), (dict(base=math.nan), absb.ERR_BAD_SHAPE), (dict(base=math.inf), absb.ERR_BAD_SHAPE),
+    (dict(scaling=1, factor=0.5), absb.ERR_BAD_SHAPE), (dict(scaling=1, factor=math.nan), absb.ERR_BAD_SHAPE),
+    (dict(scaling=2, factor=2.0, rot_dim=2), absb.ERR_BAD_SHAPE), (dict(amplitude=math.nan), absb.ERR_BAD_SHAPE),
+    (dict(scaling=3, factor=2.0, original_len=0.0, low_turns=1.0, high_turns=4.0), absb.ERR_BAD_SHAPE),
+    (dict(scaling=3, factor=2.0, original_len=99.0, low_turns=4.0, high_turns=4.0), absb.ERR_BAD_SHAPE),
+    (dict(scaling=3, factor=2.0, original_len=99.0, low_turns=-1.0, high_turns=4.0), absb.ERR_BAD_SHAPE),
+])
+def test_frequencies_refusals(kw, status):
+    with pytest.raises(absb.AbsbError) as e:
+        absb.absb_rope_frequencies(absb.Rope(**kw))
+    assert e.value.status == status
+
+
+# ------------------------------------------------------------------ refusals
+class _T:
+    """Stands for a dense device tensor of whole rows."""
+
+    def __init__(self, *shape, at=AT, stride0=None, size=2):
+        self.shape, self._at, self._s0, self._size = shape, at, stride0, size
+
+    def data_ptr(self):
+        return self._at
+
+    def numel(self):
+        return math.prod(self.shape)
+
+    def element_size(self):
+        return self._size
+
+    def dim(self):
+        return len(self.shape)
+
+    def stride(self, i):
+        dense = math.prod(self.shape[i + 1:])
+        return self._s0 if i == 0 and self._s0 is not None else dense
+
+    def is_contiguous(self):
+        return self._s0 is None
+
+
+def _map(layer=None, batch=None, before=AT, table=AT, off=AT, pos=None, slot=None, ring=None, **kw):
+    return (layer or _layer(), batch or _batch([5]), before, table, off, pos or _T(4), slot or _T(4), ring)
+
+
+def test_map_rows_refusals():
+    f = absb.absb_map_rows
+    _refused(absb.ERR_BAD_SHAPE, f, *_map(layer=_layer(page_size=12)))
+    _refused(absb.ERR_NULL, f, *_map(before=None))
+    _refused(absb.ERR_NULL, f, *_map(table=None))
+    _refused(absb.ERR_NULL, f, *_map(off=None))
+    _refused(absb.ERR_NULL, f, *_map(pos=_T(4, at=None)))
+    _refused(absb.ERR_BAD_SHAPE, f, *_map(pos=_T(5)))
+    _refused(absb.ERR_NULL, f, *_map(batch=absb.Batch(seq_lens_host=[5], pt_stride=1)))
+    _refused(absb.ERR_BAD_SHAPE, f, *_map(batch=_batch([1] * 65536)))
+    _refused(absb.ERR_BAD_SHAPE, f, *_map(batch=_batch([5], width=-1)))
+    _refused(absb.ERR_BAD_SHAPE, f, *_map(ring=absb.PageRing(_T(0), _T(4))))
+    _refused(absb.ERR_NULL, f, *_map(ring=absb.PageRing(_T(9), _T(4, at=None))))
+    lib = absb.load()
+    assert lib.absb_map_rows(None, None, None, None, None, 0, None, None, None, None) == absb.ERR_NULL
+
+
+def _rot(n=3, **kw):
+    d = dict(layer=_layer(), rope=absb.Rope(), row_pos=_T(n), row_slot=_T(n), freq=AT, q=_T(n, 32, D), q_out=_T(n, 32, D, at=AT + 4096),
+             k=_T(n, 8, D), v=_T(n, 8, D), k_cache=AT, v_cache=AT)
+    d.update(kw)
+    return d
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(layer=_layer(head_dim=64)), absb.ERR_UNSUPPORTED), (dict(layer=_layer(num_q_heads=72), q=_T(3, 72, D), q_out=_T(3, 72, D)), absb.ERR_UNSUPPORTED),
+    (dict(layer=_layer(dtype=3)), absb.ERR_UNSUPPORTED), (dict(layer=_layer(kv_strides=(4, 4, 4))), absb.ERR_BAD_SHAPE),
+    (dict(layer=_layer(kv_strides=(8 * 64 * D, 64 * D, (1 << 28) + 8))), absb.ERR_UNSUPPORTED),
+    (dict(rope=absb.Rope(rot_dim=7)), absb.ERR_BAD_SHAPE), (dict(row_pos=_T(3, at=None)), absb.ERR_NULL), (dict(row_slot=None), absb.ERR_NULL),
+    (dict(freq=None), absb.ERR_NULL), (dict(q=None), absb.ERR_NULL), (dict(q_out=None), absb.ERR_NULL), (dict(k=None), absb.ERR_NULL),
+    (dict(v=None), absb.ERR_NULL), (dict(k_cache=None), absb.ERR_NULL), (dict(v_cache=None), absb.ERR_NULL),
+    (dict(q=None, q_out=None, k=None, v=None), absb.ERR_NULL),
+    (dict(q=_T(3, 32, D, stride0=32 * D + 4)), absb.ERR_BAD_SHAPE), (dict(k=_T(3, 8, D, stride0=8 * D - 8)), absb.ERR_BAD_SHAPE),
+    (dict(v=_T(3, 8, D, stride0=8 * D + 1)), absb.ERR_BAD_SHAPE), (dict(q=_T(3, 32, D, at=AT + 8)), absb.ERR_BAD_SHAPE),
+    (dict(k_cache=AT + 2), absb.ERR_BAD_SHAPE), (dict(q=_T(3, 32, D, at=AT + 4096, stride0=48 * D)), absb.ERR_BAD_SHAPE),     # in place, rows apart
+    (dict(q=_T(4, 32, D)), absb.ERR_BAD_SHAPE), (dict(q=_T(3, 31, D)), absb.ERR_BAD_SHAPE), (dict(q_out=_T(3, 32, D, stride0=8192)), absb.ERR_BAD_SHAPE),
+])
+def test_rotate_store_refusals(kw, status):
+    _refused(status, absb.absb_rotate_store, **_rot(**kw))
+
+
+def test_rotate_store_of_no_rows_does_nothing():
+    absb.absb_rotate_store(stream=0, **_rot(n=0))
+
+
+def _att(lens=(100, 200), new=(1, 2), layer=None, batch=None, rows=None, q=AT, k=AT, v=AT, out=AT, opts=None, ws=None, **kw):
+    return (layer or _layer(), batch or _batch(lens), rows or _rows(new), q, k, v, out, None, opts, ws)
+
+
+BIG_WS = _T(1 << 40, size=1)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(layer=_layer(head_dim=64)), absb.ERR_UNSUPPORTED), (dict(layer=_layer(num_q_heads=33)), absb.ERR_BAD_SHAPE),
+    (dict(layer=_layer(num_q_heads=72)), absb.ERR_UNSUPPORTED), (dict(layer=_layer(sm_scale=-1.0)), absb.ERR_BAD_SHAPE),
+    (dict(layer=_layer(page_size=4)), absb.ERR_BAD_SHAPE), (dict(layer=_layer(kv_strides=(8, 8, (1 << 28) + 8))), absb.ERR_UNSUPPORTED),
+    (dict(new=(101, 1)), absb.ERR_BAD_SHAPE), (dict(lens=(0, 5), new=(1, 1)), absb.ERR_BAD_SHAPE), (dict(lens=(-1, 5), new=(0, 1)), absb.ERR_BAD_SHAPE),
+    (dict(rows=absb.Rows([1, 2, 3], AT)), absb.ERR_BAD_SHAPE), (dict(rows=absb.Rows([0, 2, 1], AT)), absb.ERR_BAD_SHAPE),
+    (dict(rows=absb.Rows(None, AT)), absb.ERR_NULL), (dict(rows=absb.Rows([0, 1, 2], None)), absb.ERR_NULL),
+    (dict(batch=_batch((100, 200), width=3)), absb.ERR_BAD_SHAPE),
+    (dict(q=None), absb.ERR_NULL), (dict(k=None), absb.ERR_NULL), (dict(v=None), absb.ERR_NULL), (dict(out=None), absb.ERR_NULL),
+    (dict(q=AT + 8), absb.ERR_BAD_SHAPE), (dict(out=AT + 2), absb.ERR_BAD_SHAPE), (dict(k=AT + 4), absb.ERR_BAD_SHAPE),
+    (dict(opts=absb.ScoreOpts(softcap=-1.0)), absb.ERR_BAD_SHAPE), (dict(opts=absb.ScoreOpts(softcap=math.nan)), absb.ERR_BAD_SHAPE),
+    (dict(opts=absb.ScoreOpts(softcap=math.inf)), absb.ERR_BAD_SHAPE), (dict(opts=absb.ScoreOpts(window=-1)), absb.ERR_BAD_SHAPE),
+    (dict(lens=(5000, 9000)), absb.ERR_WORKSPACE), (dict(lens=(5000, 9000), ws=_T(100, size=1)), absb.ERR_WORKSPACE),
+    (dict(lens=(5000, 9000), ws=_T(1 << 40, at=AT + 16, size=1)), absb.ERR_WORKSPACE),
+])
+def test_attend_rows_refusals(kw, status):
+    _refused(status, absb.absb_attend_rows, *_att(**kw))
+
+
+@pytest.mark.parametrize("shared,status", [
+    (absb.SharedPrefix([0, 2], [65], AT, AT), absb.ERR_BAD_SHAPE),            # not whole pages
+    (absb.SharedPrefix([0, 2], [-64], AT, AT), absb.ERR_BAD_SHAPE),
+    (absb.SharedPrefix([0, 2], [128], AT, AT), absb.ERR_BAD_SHAPE),           # longer than the first request's older tokens
+    (absb.SharedPrefix([0, 1], [64], AT, AT), absb.ERR_BAD_SHAPE),            # a request without a group
+    (absb.SharedPrefix([1, 2], [64], AT, AT), absb.ERR_BAD_SHAPE),
+    (absb.SharedPrefix([0, 2, 1, 2], [0, 0, 0], AT, AT), absb.ERR_BAD_SHAPE),
+    (absb.SharedPrefix([0, 3, 2], [0, 0], AT, AT), absb.ERR_BAD_SHAPE),
+    (absb.SharedPrefix([0, 2], [64], None, AT), absb.ERR_NULL), (absb.SharedPrefix([0, 2], [64], AT, None), absb.ERR_NULL),
+])
+def test_attend_shared_refusals(shared, status):
+    layer, batch, rows, q, k, v, out, lse, opts, _ = _att()
+    _refused(status, absb.absb_attend_shared, layer, batch, rows, shared, q, k, v, out, lse, opts, BIG_WS)
+
+
+def test_attend_refuses_null_records():
+    lib = absb.load()
+    cl, cb, cr = _layer().c(), _batch([5]).c(), _rows([1]).c()
+    n = C.c_size_t(0)
+    assert lib.absb_attend_workspace(None, C.byref(cb), C.byref(cr), None, C.byref(n)) == absb.ERR_NULL
+    assert lib.absb_attend_workspace(C.byref(cl), None, C.byref(cr), None, C.byref(n)) == absb.ERR_NULL
+    assert lib.absb_attend_workspace(C.byref(cl), C.byref(cb), None, None, C.byref(n)) == absb.ERR_NULL
+    assert lib.absb_attend_workspace(C.byref(cl), C.byref(cb), C.byref(cr), None, None) == absb.ERR_NULL
+    assert lib.absb_attend_shared(C.byref(cl), C.byref(cb), C.byref(cr), None, AT, AT, AT, AT, None, None, None, 0, None) == absb.ERR_NULL
+
+
+def test_attend_of_no_rows_does_nothing():
+    absb.absb_attend_rows(*_att(new=(0, 0)), stream=0)
+    absb.absb_attend_rows(*_att(lens=(0, 0), new=(0, 0), q=None, out=None), stream=0)
+
+
+# ------------------------------------------------------------------ workspaces
+@pytest.mark.parametrize("lens,new", [([131072], [1]), ([4096], [4096]), ([9000, 17, 4000], [1, 1, 1]), ([131072] + [100] * 63, [1] * 64),
+                                      ([2048], [1]), ([30000, 30000], [40, 3])])
+def test_workspace_sizes(lens, new):
+    # at most 65 parts a row and query head, of 128 outputs, a maximum and a sum
+    size = absb.absb_attend_workspace(_layer(), _batch(lens), _rows(new))
+    assert size % 256 == 0 and size <= sum(new) * 32 * 65 * 520 + 512
+    shared = absb.SharedPrefix([0, len(lens)], [0], AT, AT)       # nothing shared: the same call
+    assert absb.absb_attend_workspace(_layer(), _batch(lens), _rows(new), shared) == size
