@@ -38,7 +38,7 @@ struct AttendParams {
   int32_t batch, groups, pt_stride, Hq, Hkv, G, log2_page;
   int32_t window, parts, part0;   // part0: of this phase's first split
   float scale_log2;               // sm_scale * log2(e)
-  float cap_log2, cap_in;         // cap * log2(e), sm_scale / cap (capped only)
+  float cap_log2, cap_in;         // cap * log2(e), 2 log2(e) sm_scale / cap (capped only)
   int32_t cap_wide;               // 1: the cap is so far above ordinary scores that small ones need the series
   AttendPhase phase;
 };

@@ -88,25 +88,19 @@ struct State {
   f32x16 o[4];
 };
 
-// Scores in log2 units, from S = q.k: the cap, then the distance bias.
-template <bool CAP, bool BIAS>
-__device__ __forceinline__ float score_of(const AttendParams& p, float s, float slope_log2, int pos, int key) {
-  float x;
-  if (CAP) {
-    // cap tanh(y) = cap - 2 cap / (e^2y + 1), off by 2^-23 cap; where that is too much, small y by the series
-    const float y = s * p.cap_in, t = exp2_fast(y * (2.0f * LOG2E));
-    x = __builtin_fmaf(-2.0f * p.cap_log2, __builtin_amdgcn_rcpf(t + 1.0f), p.cap_log2);
-    if (p.cap_wide) {
-      const float z = y * y;
-      const float series = y * (1.0f + z * (-1.0f / 3 + z * (2.0f / 15 + z * (-17.0f / 315 + z * (62.0f / 2835)))));
-      x = __builtin_fabsf(y) < 0.25f ? series * p.cap_log2 : x;
-    }
-  } else {
-    x = s * p.scale_log2;
-  }
-  if (BIAS) x -= slope_log2 * (float)__builtin_abs(pos - key);
-  return x;
+// cap tanh(y), in log2 units: cap - 2 cap / (e^2y + 1) is off by 2^-23 cap at most.
+__device__ __forceinline__ float capped(const AttendParams& p, float s) {
+  const float t = exp2_fast(s * p.cap_in);
+  return __builtin_fmaf(-2.0f * p.cap_log2, __builtin_amdgcn_rcpf(t + 1.0f), p.cap_log2);
 }
+// ... where that is too much (large caps), small y by the series.
+__device__ __forceinline__ float capped_wide(const AttendParams& p, float s) {
+  const float y = s * p.cap_in * (0.5f * LN2), z = y * y;
+  const float series = y * (1.0f + z * (-1.0f / 3 + z * (2.0f / 15 + z * (-17.0f / 315 + z * (62.0f / 2835)))));
+  return __builtin_fabsf(y) < 0.25f ? series * p.cap_log2 : capped(p, s);
+}
+// Keeps the compiler from making a branch that hardly any block takes into selects that every block pays for.
+__device__ __forceinline__ void rarely() { asm volatile(""); }
 
 // 32 KT keys in LDS (K's rows at `kl`, V's at `vl`) folded into the state.  `k0`: the first one's index; MASK: some row of
 // the wave does not see all of them.
@@ -125,17 +119,35 @@ __device__ __forceinline__ void fold_keys(const AttendParams& p, const char* kl,
       s[t] = mma_32x32x16<DT>(a, q[c], s[t]);
     }
   }
+  const int first_key = k0 + 4 * half;  // score i of tile t is of key first_key + 32 t + 8 (i / 4) + i % 4
+  auto each = [&](auto f) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < KT; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[t][i] = f(s[t][i], 32 * t + 8 * (i >> 2) + (i & 3));
+  };
+  if (CAP) {
+    if (p.cap_wide) {
+      rarely();
+      each([&](float x, int) { return capped_wide(p, x); });
+    } else {
+      each([&](float x, int) { return capped(p, x); });
+    }
+  }
+  if (BIAS) {
+    const float d = (float)(row.pos - first_key);  // (exact below 2^24 tokens; beyond, distances are off by a part in 2^24)
+    each([&](float x, int at) { return __builtin_fmaf(-slope_log2, __builtin_fabsf(d - (float)at), CAP ? x : x * p.scale_log2); });
+  }
+  if (mask) {
+    rarely();
+    const int lo = row.lo - first_key, hi = row.hi - first_key;
+    each([&](float x, int at) { return at >= lo && at <= hi ? x : -__builtin_inff(); });
+  }
   float mx = -__builtin_inff();
 #pragma unroll
   for (int t = 0; t < KT; ++t)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int key = k0 + 32 * t + 8 * (i >> 2) + 4 * half + (i & 3);
-      float x = (CAP || BIAS) ? score_of<CAP, BIAS>(p, s[t][i], slope_log2, row.pos, key) : s[t][i];
-      if (mask) x = key >= row.lo && key <= row.hi ? x : -__builtin_inff();
-      s[t][i] = x;
-      mx = fmaxf(mx, x);
-    }
+    for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[t][i]);
   mx = across_halves(mx, [](float a, float b) { return fmaxf(a, b); });
   constexpr bool SCALED = CAP || BIAS;  // (else the scores are still q.k)
   const float mn = fmaxf(st.m, SCALED ? mx : mx * p.scale_log2);
@@ -195,18 +207,28 @@ __device__ __forceinline__ Stretch look_up(const AttendParams& p, const int32_t*
   return s;
 }
 
+// 16 bytes a lane from `base` (+ a lane's 32-bit offset) to LDS, lanes side by side from `to` on.  As the instruction itself: the
+// compiler would wait for every copy in flight ahead of every read of LDS, the one of the next block included.  (It must wait
+// for none: copies_done() does, in front of the barrier behind which a block is read.  The waits: m0 wants one state ahead of the
+// copy, a scalar that came from a vector instruction five.)
+__device__ __forceinline__ void copy_to_lds(const char* base, uint32_t lane_off, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(lane_off), "s"(base) : "memory");
+}
+__device__ __forceinline__ uint32_t lds_address(const char* at) {
+  typedef __attribute__((address_space(3))) const char* lds;
+  return (uint32_t)(uintptr_t)(lds)(at);
+}
+
 // Copies rows 4 i .. 4 i + 3 of the wave's rows of a block to LDS: eight keys' offset and last row from lane `from` of the
-// stretch, the upper four of them if `upper`.
+// stretch, the upper four of them if `i` is odd.
 __device__ __forceinline__ void copy_rows(const AttendParams& p, const char* k, const char* v, const Stretch& s, int from, int i,
-                                          char* kl, char* vl) {
+                                          uint32_t kl, uint32_t vl) {
   const int lane = threadIdx.x & 63, piece = lane & 15, r4 = lane >> 4;
   const uint64_t off = lane_u64(s.off, from);
   const int most = __builtin_amdgcn_readlane(s.most, from);
-  const uint64_t row = off + (uint64_t)min(4 * (i & 1) + r4, most) * (uint64_t)p.s_tok;
-  typedef __attribute__((address_space(1))) const void* gptr;
-  typedef __attribute__((address_space(3))) void* lptr;
-  __builtin_amdgcn_global_load_lds((gptr)(k + row + ((piece ^ (4 * (i & 3) + r4)) * 16)), (lptr)(kl + 4 * i * ROW_BYTES), 16, 0, 0);
-  __builtin_amdgcn_global_load_lds((gptr)(v + row + ((piece ^ (r4 << 2)) * 16)), (lptr)(vl + 4 * i * ROW_BYTES), 16, 0, 0);
+  const uint32_t row = (uint32_t)min(4 * (i & 1) + r4, most) * (uint32_t)p.s_tok;  // (7 rows of at most 2^29 bytes)
+  copy_to_lds(k + off, row + (uint32_t)((piece ^ (4 * (i & 3) + r4)) * 16), kl + 4 * i * ROW_BYTES);
+  copy_to_lds(v + off, row + (uint32_t)((piece ^ (r4 << 2)) * 16), vl + 4 * i * ROW_BYTES);
 }
 
 // The wave's copies have arrived, and what it read of LDS has, too (the next copy may overwrite it).
@@ -321,9 +343,10 @@ __global__ __launch_bounds__(ATT_THREADS, WIDE ? 2 : 1) void attend_kernel(Atten
     constexpr int STEP = WIDE ? 64 : 128;
     const int steps = (end - begin + STEP - 1) / STEP;
     Stretch now = look_up(p, pages, begin, t.limit), next = now;
-    char* mine = WIDE ? s_kv : s_kv + wave * 4 * STAGE;
+    const char* mine = WIDE ? s_kv : s_kv + wave * 4 * STAGE;
+    const uint32_t mine_lds = lds_address(mine);
     auto copy = [&](int i, int buf) __attribute__((always_inline)) {
-      char *kl = mine + buf * 2 * STAGE, *vl = kl + STAGE;
+      uint32_t kl = mine_lds + buf * 2 * STAGE, vl = kl + STAGE;
       const Stretch& s = now;
       if (WIDE) {
         kl += 16 * wave * ROW_BYTES;
