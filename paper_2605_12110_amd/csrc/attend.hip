@@ -13,6 +13,8 @@
 // K and V are copied from their pages straight to LDS, a block ahead, 16 bytes a lane.  The copy writes lanes side by side, so
 // what spreads a read over the banks is which piece of a row a lane fetches: K's piece p of row r lies at p ^ (r % 16), V's at
 // p ^ 4 (r % 4).
+#include <type_traits>
+
 #include "attend.h"
 
 namespace absb {
@@ -102,24 +104,26 @@ __device__ __forceinline__ float capped_wide(const AttendParams& p, float s) {
 // Keeps the compiler from making a branch that hardly any block takes into selects that every block pays for.
 __device__ __forceinline__ void rarely() { asm volatile(""); }
 
-// 32 KT keys in LDS (K's rows at `kl`, V's at `vl`) folded into the state.  `k0`: the first one's index; MASK: some row of
-// the wave does not see all of them.
-template <int DT, bool CAP, bool BIAS, int KT>
-__device__ __forceinline__ void fold_keys(const AttendParams& p, const char* kl, const char* vl, int k0, bool mask, const u32x4 (&q)[8],
-                                          const RowOf& row, float slope_log2, State& st) {
+// S^T of the 32 keys whose K rows are at `kl`: score i of a lane is of key 8 (i / 4) + 4 half + i % 4.
+template <int DT>
+__device__ __forceinline__ f32x16 scores_of(const char* kl, const u32x4 (&q)[8]) {
   const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
-  f32x16 s[KT];
+  f32x16 s;
 #pragma unroll
-  for (int t = 0; t < KT; ++t) {
+  for (int i = 0; i < 16; ++i) s[i] = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
-#pragma unroll
-    for (int c = 0; c < 8; ++c) {
-      const u32x4 a = *reinterpret_cast<const u32x4*>(kl + (32 * t + col) * ROW_BYTES + (((2 * c + half) ^ (col & 15)) * 16));
-      s[t] = mma_32x32x16<DT>(a, q[c], s[t]);
-    }
+  for (int c = 0; c < 8; ++c) {
+    const u32x4 a = *reinterpret_cast<const u32x4*>(kl + col * ROW_BYTES + (((2 * c + half) ^ (col & 15)) * 16));
+    s = mma_32x32x16<DT>(a, q[c], s);
   }
-  const int first_key = k0 + 4 * half;  // score i of tile t is of key first_key + 32 t + 8 (i / 4) + i % 4
+  return s;
+}
+
+// Scores of 32 KT keys from `k0` on, as products, made into what the softmax takes: in log2 units with a cap or a bias (else times
+// scale_log2, which the weights do), and -inf where a row does not see a key.  `mask`: some row of the wave does not.
+template <bool CAP, bool BIAS, int KT>
+__device__ __forceinline__ void adjust(const AttendParams& p, f32x16 (&s)[KT], int k0, bool mask, const RowOf& row, float slope_log2) {
+  const int first_key = k0 + 4 * ((threadIdx.x & 63) >> 5);
   auto each = [&](auto f) __attribute__((always_inline)) {
 #pragma unroll
     for (int t = 0; t < KT; ++t)
@@ -143,35 +147,62 @@ __device__ __forceinline__ void fold_keys(const AttendParams& p, const char* kl,
     const int lo = row.lo - first_key, hi = row.hi - first_key;
     each([&](float x, int at) { return at >= lo && at <= hi ? x : -__builtin_inff(); });
   }
+}
+
+// The maximum that the rows' weights are taken against.  It follows the scores' own only when they exceed it by 2^RISE:
+// weights then reach 2^RISE, which the K/V types hold as exactly as those below 1, and the output is hardly ever scaled again
+// (with the true maximum some of a wave's 32 rows has a new one in most blocks).
+constexpr float RISE = 8.0f;
+template <int KT>
+__device__ __forceinline__ float largest(const f32x16 (&s)[KT]) {
   float mx = -__builtin_inff();
 #pragma unroll
   for (int t = 0; t < KT; ++t)
 #pragma unroll
     for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[t][i]);
+  return mx;
+}
+template <bool SCALED>
+__device__ __forceinline__ float new_maximum(const AttendParams& p, float mx, State& st) {
   mx = across_halves(mx, [](float a, float b) { return fmaxf(a, b); });
-  constexpr bool SCALED = CAP || BIAS;  // (else the scores are still q.k)
-  const float mn = fmaxf(st.m, SCALED ? mx : mx * p.scale_log2);
-  const float base = mn == -__builtin_inff() ? 0.0f : mn;  // nothing seen yet: weights 0, not NaN
-  const float alpha = exp2_fast(st.m - base);
-  st.m = mn;
-  float sum = 0.0f;
-#pragma unroll
-  for (int t = 0; t < KT; ++t)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      s[t][i] = exp2_fast(SCALED ? s[t][i] - base : __builtin_fmaf(s[t][i], p.scale_log2, -base));
-      sum += s[t][i];
-    }
-  st.l = __builtin_fmaf(st.l, alpha, sum);
-  if (__any(alpha != 1.0f)) {
+  if (!SCALED) mx *= p.scale_log2;
+  const bool rises = mx > st.m + RISE;  // (the first key seen: above -inf)
+  if (__any(rises)) {
+    rarely();
+    const float mn = rises ? mx : st.m;
+    const float alpha = rises ? exp2_fast(st.m - mn) : 1.0f;
+    st.m = mn;
+    st.l *= alpha;
 #pragma unroll
     for (int t = 0; t < 4; ++t) st.o[t] *= alpha;
   }
+  return st.m == -__builtin_inff() ? 0.0f : st.m;  // nothing seen yet: weights 0, not NaN
+}
+
+// Weights of the scores, rounded to the K/V type (two to a word: P^T as the product takes it), and their sum before rounding.
+template <int DT, bool SCALED, int KT>
+__device__ __forceinline__ void weigh(const AttendParams& p, const f32x16 (&s)[KT], float base, u32x4 (&w)[2 * KT], State& st) {
+  float sum = 0.0f;
+#pragma unroll
+  for (int c = 0; c < 2 * KT; ++c)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float a = s[c >> 1][8 * (c & 1) + 2 * j], b = s[c >> 1][8 * (c & 1) + 2 * j + 1];
+      const float x = exp2_fast(SCALED ? a - base : __builtin_fmaf(a, p.scale_log2, -base));
+      const float y = exp2_fast(SCALED ? b - base : __builtin_fmaf(b, p.scale_log2, -base));
+      sum += x;
+      sum += y;
+      w[c][j] = pack2<DT>(x, y);
+    }
+  st.l += sum;
+}
+
+// O^T += V^T P^T for the 32 KT keys whose V rows are at `vl`.
+template <int DT, int KT>
+__device__ __forceinline__ void add_values(const char* vl, const u32x4 (&w)[2 * KT], State& st) {
+  const int lane = threadIdx.x & 63, half = lane >> 5;
 #pragma unroll
   for (int c = 0; c < 2 * KT; ++c) {
-    u32x4 w;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) w[j] = pack2<DT>(s[c >> 1][8 * (c & 1) + 2 * j], s[c >> 1][8 * (c & 1) + 2 * j + 1]);
     // V^T: of 16 lanes, lane i points at channels 4 (i % 4).. of key i / 4 and gets channel i of the four keys
     const int i16 = lane & 15, grp = (lane >> 4) & 1, key = 16 * c + 4 * half + (i16 >> 2);
 #pragma unroll
@@ -181,9 +212,69 @@ __device__ __forceinline__ void fold_keys(const AttendParams& p, const char* kl,
       typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
       const u32x2 lo = bitcast<u32x2>(__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(at)));
       const u32x2 hi = bitcast<u32x2>(__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(at + 8 * ROW_BYTES)));
-      st.o[t] = mma_32x32x16<DT>(u32x4{lo[0], lo[1], hi[0], hi[1]}, w, st.o[t]);
+      st.o[t] = mma_32x32x16<DT>(u32x4{lo[0], lo[1], hi[0], hi[1]}, w[c], st.o[t]);
     }
   }
+}
+
+// The main part of a step of a wide tile, in an order of its own (the compiler's would wait for every read of LDS right before its
+// product): 16 products of the next block's scores, then 16 of this block's weights with its values; beside each, the vector work
+// of one score or two, and the read that the fourth product after it needs.  A product takes the matrix unit 32 cycles, an
+// exponential the vector unit 16, its other work 12.  `mx`: the largest of a lane's next scores.
+template <int DT, bool SCALED>
+__device__ __forceinline__ void wide_step(const AttendParams& p, const char* kl, const char* vl, const u32x4 (&q)[8], const f32x16 (&s)[2],
+                                          float base, f32x16 (&s_next)[2], float& mx, State& st) {
+  constexpr int AHEAD = 4, SLOTS = 32;
+  const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5, i16 = lane & 15, grp = (lane >> 4) & 1;
+  u32x4 f[AHEAD], w[4];
+  float x = 0.0f, sum0 = 0.0f, sum1 = 0.0f;
+  mx = -__builtin_inff();
+  auto fetch = [&](int j) __attribute__((always_inline)) {  // the operand of product j
+    if (j < 16) {
+      const int t = j & 1, c = j >> 1;
+      f[j % AHEAD] = *reinterpret_cast<const u32x4*>(kl + (32 * t + col) * ROW_BYTES + (((2 * c + half) ^ (col & 15)) * 16));
+    } else {
+      // V^T: of 16 lanes, lane i points at channels 4 (i % 4).. of key i / 4 and gets channel i of the four keys
+      const int c = (j - 16) >> 2, t = j & 3, key = 16 * c + 4 * half + (i16 >> 2);
+      const int piece = (4 * t + 2 * grp + ((i16 & 3) >> 1)) ^ ((key & 3) << 2);
+      const char* at = vl + key * ROW_BYTES + piece * 16 + (i16 & 1) * 8;
+      typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
+      const u32x2 lo = bitcast<u32x2>(__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(at)));
+      const u32x2 hi = bitcast<u32x2>(__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(at + 8 * ROW_BYTES)));
+      f[j % AHEAD] = u32x4{lo[0], lo[1], hi[0], hi[1]};
+    }
+  };
+#pragma unroll
+  for (int j = 0; j < AHEAD; ++j) fetch(j);
+  const f32x16 zero = {};
+#pragma unroll
+  for (int j = 0; j < SLOTS; ++j) {
+    if (j < 16)
+      s_next[j & 1] = mma_32x32x16<DT>(f[j % AHEAD], q[j >> 1], j < 2 ? zero : s_next[j & 1]);
+    else
+      st.o[j & 3] = mma_32x32x16<DT>(f[j % AHEAD], w[(j - 16) >> 2], st.o[j & 3]);
+    if (j + AHEAD < SLOTS) fetch(j + AHEAD);
+    // 32 weights in 28 slots: those of 16 keys are there before their product
+#pragma unroll
+    for (int e = j * 8 / 7; e < (j + 1) * 8 / 7 && e < 32; ++e) {
+      const float a = s[e >> 4][e & 15];
+      const float y = exp2_fast(SCALED ? a - base : __builtin_fmaf(a, p.scale_log2, -base));
+      if (e & 1) {
+        sum1 += y;
+        w[e >> 3][(e & 7) >> 1] = pack2<DT>(x, y);
+      } else {
+        sum0 += y;
+        x = y;
+      }
+    }
+    if (!SCALED && j >= 20 && j < 28) {
+#pragma unroll
+      for (int e = (j - 20) * 4; e < (j - 19) * 4; ++e) mx = fmaxf(mx, s_next[e >> 4][e & 15]);
+    }
+    asm volatile("" : "+v"(sum0), "+v"(sum1));  // (the sums are made here, not out of 32 kept values at the end)
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  st.l += sum0 + sum1;
 }
 
 __device__ __forceinline__ uint64_t lane_u64(uint64_t v, int lane) {
@@ -192,17 +283,22 @@ __device__ __forceinline__ uint64_t lane_u64(uint64_t v, int lane) {
 }
 
 // Where the rows of 512 keys lie: lane j of the wave has the byte offset of keys 8 j .. 8 j + 7 of the stretch (they share a
-// page) and which of the eight is the last that exists.
+// page) and which of the eight is the last that exists.  In two halves: the page is asked for a stretch ahead, and the
+// offset worked out when the stretch begins.
 struct Stretch {
   uint64_t off;
   int most;
 };
-__device__ __forceinline__ Stretch look_up(const AttendParams& p, const int32_t* pages, int k0, int limit) {
-  const int lane = threadIdx.x & 63;
-  const int key = min((int64_t)k0 + 8 * lane, (int64_t)limit - 1), at = key & ~7;
+__device__ __forceinline__ int first_of_lane(int k0, int limit) {
+  return (int)min((int64_t)k0 + 8 * (threadIdx.x & 63), (int64_t)limit - 1) & ~7;
+}
+__device__ __forceinline__ int32_t ask_page(const AttendParams& p, const int32_t* pages, int k0, int limit) {
+  return pages[first_of_lane(k0, limit) >> p.log2_page];
+}
+__device__ __forceinline__ Stretch stretch_on(const AttendParams& p, int32_t page, int k0, int limit) {
+  const int at = first_of_lane(k0, limit);
   Stretch s;
-  s.off = (uint64_t)pages[at >> p.log2_page] * (uint64_t)p.s_page +
-          (uint64_t)(at & ((1 << p.log2_page) - 1)) * (uint64_t)p.s_tok;
+  s.off = (uint64_t)page * (uint64_t)p.s_page + (uint64_t)(at & ((1 << p.log2_page) - 1)) * (uint64_t)p.s_tok;
   s.most = min(7, limit - 1 - at);
   return s;
 }
@@ -221,14 +317,12 @@ __device__ __forceinline__ uint32_t lds_address(const char* at) {
 
 // Copies rows 4 i .. 4 i + 3 of the wave's rows of a block to LDS: eight keys' offset and last row from lane `from` of the
 // stretch, the upper four of them if `i` is odd.
-__device__ __forceinline__ void copy_rows(const AttendParams& p, const char* k, const char* v, const Stretch& s, int from, int i,
-                                          uint32_t kl, uint32_t vl) {
+__device__ __forceinline__ void copy_rows(const AttendParams& p, const char* base, const Stretch& s, int from, int i, uint32_t to, bool key) {
   const int lane = threadIdx.x & 63, piece = lane & 15, r4 = lane >> 4;
   const uint64_t off = lane_u64(s.off, from);
   const int most = __builtin_amdgcn_readlane(s.most, from);
   const uint32_t row = (uint32_t)min(4 * (i & 1) + r4, most) * (uint32_t)p.s_tok;  // (7 rows of at most 2^29 bytes)
-  copy_to_lds(k + off, row + (uint32_t)((piece ^ (4 * (i & 3) + r4)) * 16), kl + 4 * i * ROW_BYTES);
-  copy_to_lds(v + off, row + (uint32_t)((piece ^ (r4 << 2)) * 16), vl + 4 * i * ROW_BYTES);
+  copy_to_lds(base + off, row + (uint32_t)((piece ^ (key ? 4 * (i & 3) + r4 : r4 << 2)) * 16), to + 4 * i * ROW_BYTES);
 }
 
 // The wave's copies have arrived, and what it read of LDS has, too (the next copy may overwrite it).
@@ -339,41 +433,98 @@ __global__ __launch_bounds__(ATT_THREADS, WIDE ? 2 : 1) void attend_kernel(Atten
     const float slope_log2 = BIAS && valid ? p.slopes[row.head] * LOG2E : 0.0f;
     const int32_t* pages = p.page_table + (int64_t)t.table_row * p.pt_stride;
     const char *kb = p.k + kv_head * p.s_head, *vb = p.v + kv_head * p.s_head;
-    // Stretches of 512 keys from `begin` on; a step is 64 keys (WIDE), or 128, 32 a wave.
-    constexpr int STEP = WIDE ? 64 : 128;
+    constexpr bool SCALED = CAP || BIAS;
+    constexpr int STEP = WIDE ? 64 : 128;  // keys of a step; narrow: 32 a wave
+    constexpr int PER = 512 / STEP;        // steps of a stretch
     const int steps = (end - begin + STEP - 1) / STEP;
-    Stretch now = look_up(p, pages, begin, t.limit), next = now;
     const char* mine = WIDE ? s_kv : s_kv + wave * 4 * STAGE;
     const uint32_t mine_lds = lds_address(mine);
-    auto copy = [&](int i, int buf) __attribute__((always_inline)) {
-      uint32_t kl = mine_lds + buf * 2 * STAGE, vl = kl + STAGE;
-      const Stretch& s = now;
+    auto stretch_begin = [&](int n) { return (int)min((int64_t)begin + (int64_t)n * 512, (int64_t)t.limit - 1); };
+    auto ask = [&](int n) { return ask_page(p, pages, stretch_begin(n), t.limit); };
+    auto stretch = [&](int n, int32_t page) { return stretch_on(p, page, stretch_begin(n), t.limit); };
+    // K, or V, of step i to its buffer i % 2 (of K's two, or V's behind them)
+    auto copy = [&](const Stretch& s, int i, const char* base, bool key) __attribute__((always_inline)) {
+      uint32_t to = mine_lds + (i & 1) * STAGE + (key ? 0 : 2 * STAGE);
       if (WIDE) {
-        kl += 16 * wave * ROW_BYTES;
-        vl += 16 * wave * ROW_BYTES;
+        to += 16 * wave * ROW_BYTES;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) copy_rows(p, kb, vb, s, (i & 7) * 8 + 2 * wave + (j >> 1), j, kl, vl);
+        for (int j = 0; j < 4; ++j) copy_rows(p, base, s, (i & 7) * 8 + 2 * wave + (j >> 1), j, to, key);
       } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) copy_rows(p, kb, vb, s, (i & 3) * 16 + 4 * wave + (j >> 1), j, kl, vl);
+        for (int j = 0; j < 8; ++j) copy_rows(p, base, s, (i & 3) * 16 + 4 * wave + (j >> 1), j, to, key);
       }
     };
-    constexpr int PER = 512 / STEP;  // steps of a stretch
-    copy(0, 0);
-    for (int i = 0; i < steps; ++i) {
+    Stretch k_at = stretch(0, ask(0)), v_at = k_at;
+    if (WIDE) {
+      // Step i: the scores of block i + 1 are worked out beside the softmax of block i, matrix and vector unit at once; so K is
+      // copied two blocks ahead, V one.  (The last step works out scores of whatever is in LDS, for nobody.)
+      copy(k_at, 0, kb, true);
+      copy(v_at, 0, vb, false);
+      int32_t next = ask(1);
       copies_done();
-      if (WIDE) __syncthreads();  // ... everybody's, and nobody reads the other buffer any more
-      if (i + 1 < steps) {
-        if ((i + 1) % PER == 0) now = next;
-        copy(i + 1, (i + 1) & 1);
-        if ((i + 1) % PER == 0 || i == 0) next = look_up(p, pages, (int)min((int64_t)begin + ((i + 1) / PER + 1) * 512, (int64_t)t.limit - 1), t.limit);
+      __syncthreads();
+      if (steps > 1) copy(k_at, 1, kb, true);
+      const bool live = wave_lo <= wave_hi;  // (waves whose rows see nothing only copy)
+      f32x16 s0[2], s1[2];
+      if (live) {
+        s0[0] = scores_of<DT>(mine, q);
+        s0[1] = scores_of<DT>(mine + 32 * ROW_BYTES, q);
       }
-      const int k0 = begin + i * STEP + (WIDE ? 0 : 32 * wave), k1 = k0 + (WIDE ? 63 : 31);
-      const char* kl = mine + (i & 1) * 2 * STAGE;
-      if (k0 > wave_hi || k1 < wave_lo) continue;
-      // a split ends on a block or with the tile's last key, so what a row sees of a block is in its interval
-      const bool mask = k0 < all_lo || k1 > all_hi;
-      fold_keys<DT, CAP, BIAS, WIDE ? 2 : 1>(p, kl, kl + STAGE, k0, mask, q, row, slope_log2, st);
+      float mx = live ? largest<2>(s0) : 0.0f;
+      auto step = [&](int i, f32x16 (&s)[2], f32x16 (&s_next)[2]) __attribute__((always_inline)) {
+        const char *kl = mine + ((i + 1) & 1) * STAGE, *vl = mine + 2 * STAGE + (i & 1) * STAGE;
+        copies_done();
+        __syncthreads();  // K of block i + 1 and V of block i are there, and nobody reads the ones before any more
+        if (i + 1 < steps) {
+          if ((i + 1) % PER == 0) v_at = k_at;
+          copy(v_at, i + 1, vb, false);
+        }
+        if (i + 2 < steps) {
+          if ((i + 2) % PER == 0) {
+            k_at = stretch((i + 2) / PER, next);
+            next = ask((i + 2) / PER + 1);
+          }
+          copy(k_at, i + 2, kb, true);
+        }
+        if (!live) return;
+        const int k0 = begin + i * STEP;
+        const bool mask = k0 < all_lo || k0 + 63 > all_hi;
+        if (SCALED || mask) {
+          rarely();
+          adjust<CAP, BIAS, 2>(p, s, k0, mask, row, slope_log2);
+          mx = largest<2>(s);
+        }
+        const float base = new_maximum<SCALED>(p, mx, st);
+        wide_step<DT, SCALED>(p, kl, vl, q, s, base, s_next, mx, st);
+      };
+      for (int i = 0; i < steps; i += 2) {
+        step(i, s0, s1);
+        if (i + 1 < steps) step(i + 1, s1, s0);
+      }
+    } else {
+      copy(k_at, 0, kb, true);
+      copy(k_at, 0, vb, false);
+      int32_t next = ask(1);
+      for (int i = 0; i < steps; ++i) {
+        copies_done();
+        if (i + 1 < steps) {
+          if ((i + 1) % PER == 0) {
+            k_at = stretch((i + 1) / PER, next);
+            next = ask((i + 1) / PER + 1);
+          }
+          copy(k_at, i + 1, kb, true);
+          copy(k_at, i + 1, vb, false);
+        }
+        const int k0 = begin + i * STEP + 32 * wave, k1 = k0 + 31;
+        if (k0 > wave_hi || k1 < wave_lo) continue;
+        // (a split ends on a block or with the tile's last key, so what a row sees of a block is in its interval)
+        f32x16 s[1] = {scores_of<DT>(mine + (i & 1) * STAGE, q)};
+        adjust<CAP, BIAS, 1>(p, s, k0, k0 < all_lo || k1 > all_hi, row, slope_log2);
+        const float base = new_maximum<SCALED>(p, largest<1>(s), st);
+        u32x4 w[2];
+        weigh<DT, SCALED, 1>(p, s, base, w, st);
+        add_values<DT, 1>(mine + 2 * STAGE + (i & 1) * STAGE, w, st);
+      }
     }
   }
   st.l = across_halves(st.l, [](float a, float b) { return a + b; });
