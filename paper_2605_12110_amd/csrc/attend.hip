@@ -315,14 +315,39 @@ __device__ __forceinline__ uint32_t lds_address(const char* at) {
   return (uint32_t)(uintptr_t)(lds)(at);
 }
 
-// Copies rows 4 i .. 4 i + 3 of the wave's rows of a block to LDS: eight keys' offset and last row from lane `from` of the
-// stretch, the upper four of them if `i` is odd.
-__device__ __forceinline__ void copy_rows(const AttendParams& p, const char* base, const Stretch& s, int from, int i, uint32_t to, bool key) {
-  const int lane = threadIdx.x & 63, piece = lane & 15, r4 = lane >> 4;
-  const uint64_t off = lane_u64(s.off, from);
-  const int most = __builtin_amdgcn_readlane(s.most, from);
-  const uint32_t row = (uint32_t)min(4 * (i & 1) + r4, most) * (uint32_t)p.s_tok;  // (7 rows of at most 2^29 bytes)
-  copy_to_lds(base + off, row + (uint32_t)((piece ^ (key ? 4 * (i & 3) + r4 : r4 << 2)) * 16), to + 4 * i * ROW_BYTES);
+// What copies of rows need of a lane: it fetches piece lane % 16 (of 16 bytes) of row lane / 16 of four, so that lanes side by
+// side in LDS hold what lies at p ^ (r % 16) of K's row r, at p ^ 4 (r % 4) of V's.
+struct LaneCopy {
+  uint32_t key[4], value[2];  // byte offsets from eight keys' first row: of K's rows 4 i .. 4 i + 3 of 16, of V's (upper four: 1)
+};
+__device__ __forceinline__ LaneCopy lane_copy(uint32_t pitch) {
+  const uint32_t lane = threadIdx.x & 63, piece = lane & 15, r4 = lane >> 4;
+  LaneCopy c;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) c.key[i] = (4 * (i & 1) + r4) * pitch + ((piece ^ (4 * i + r4)) * 16);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) c.value[i] = (4 * i + r4) * pitch + ((piece ^ (r4 << 2)) * 16);
+  return c;
+}
+// Copies N groups of eight rows, at `off` of K or V, to LDS.  `most`: the last row of each group that exists (`full`: all do); the
+// ones behind it are that row again, which no one sees.
+template <bool KEY, int N>
+__device__ __forceinline__ void copy_groups(const char* base, const uint64_t (&off)[N], const int (&most)[N], bool full, uint32_t pitch,
+                                            const LaneCopy& lc, uint32_t to) {
+  auto copy = [&](auto all) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < 2 * N; ++j) {
+      uint32_t at = KEY ? lc.key[j & 3] : lc.value[j & 1];
+      if (!decltype(all)::value) at -= (uint32_t)max(0, 4 * (j & 1) + (int)((threadIdx.x & 63) >> 4) - most[j >> 1]) * pitch;
+      copy_to_lds(base + off[j >> 1], at, to + 4 * j * ROW_BYTES);
+    }
+  };
+  if (full) {
+    copy(std::true_type());
+  } else {
+    rarely();
+    copy(std::false_type());
+  }
 }
 
 // The wave's copies have arrived, and what it read of LDS has, too (the next copy may overwrite it).
@@ -442,28 +467,47 @@ __global__ __launch_bounds__(ATT_THREADS, WIDE ? 2 : 1) void attend_kernel(Atten
     auto stretch_begin = [&](int n) { return (int)min((int64_t)begin + (int64_t)n * 512, (int64_t)t.limit - 1); };
     auto ask = [&](int n) { return ask_page(p, pages, stretch_begin(n), t.limit); };
     auto stretch = [&](int n, int32_t page) { return stretch_on(p, page, stretch_begin(n), t.limit); };
-    // K, or V, of step i to its buffer i % 2 (of K's two, or V's behind them)
-    auto copy = [&](const Stretch& s, int i, const char* base, bool key) __attribute__((always_inline)) {
-      uint32_t to = mine_lds + (i & 1) * STAGE + (key ? 0 : 2 * STAGE);
-      if (WIDE) {
-        to += 16 * wave * ROW_BYTES;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) copy_rows(p, base, s, (i & 7) * 8 + 2 * wave + (j >> 1), j, to, key);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) copy_rows(p, base, s, (i & 3) * 16 + 4 * wave + (j >> 1), j, to, key);
-      }
+    const uint32_t pitch = (uint32_t)p.s_tok;  // (seven rows of at most 2^29 bytes)
+    const LaneCopy lc = lane_copy(pitch);
+    constexpr int GROUPS = WIDE ? 2 : 4;  // of eight rows, that a wave copies of a block
+    struct Groups {
+      uint64_t off[GROUPS];
+      int most[GROUPS];
+      bool full;
     };
-    Stretch k_at = stretch(0, ask(0)), v_at = k_at;
+    // This wave's rows of step i, from the stretch that it is in.
+    auto groups = [&](const Stretch& s, int i) __attribute__((always_inline)) {
+      Groups g;
+      g.full = true;
+#pragma unroll
+      for (int j = 0; j < GROUPS; ++j) {
+        const int from = WIDE ? (i % PER) * 8 + 2 * wave + j : (i % PER) * 16 + 4 * wave + j;
+        g.off[j] = lane_u64(s.off, from);
+        g.most[j] = __builtin_amdgcn_readlane(s.most, from);
+        g.full = g.full && g.most[j] == 7;
+      }
+      return g;
+    };
+    // Its K, or V, to buffer i % 2 (of K's two, or V's behind them).
+    const uint32_t to = mine_lds + (WIDE ? 16 * wave * ROW_BYTES : 0);
+    auto copy_k = [&](const Groups& g, int i) __attribute__((always_inline)) {
+      copy_groups<true, GROUPS>(kb, g.off, g.most, g.full, pitch, lc, to + (i & 1) * STAGE);
+    };
+    auto copy_v = [&](const Groups& g, int i) __attribute__((always_inline)) {
+      copy_groups<false, GROUPS>(vb, g.off, g.most, g.full, pitch, lc, to + (2 + (i & 1)) * STAGE);
+    };
+    Stretch at = stretch(0, ask(0));
+    Groups rows = groups(at, 0);
     if (WIDE) {
       // Step i: the scores of block i + 1 are worked out beside the softmax of block i, matrix and vector unit at once; so K is
       // copied two blocks ahead, V one.  (The last step works out scores of whatever is in LDS, for nobody.)
-      copy(k_at, 0, kb, true);
-      copy(v_at, 0, vb, false);
+      copy_k(rows, 0);
+      copy_v(rows, 0);
       int32_t next = ask(1);
       copies_done();
       __syncthreads();
-      if (steps > 1) copy(k_at, 1, kb, true);
+      rows = groups(at, 1);
+      if (steps > 1) copy_k(rows, 1);
       const bool live = wave_lo <= wave_hi;  // (waves whose rows see nothing only copy)
       f32x16 s0[2], s1[2];
       if (live) {
@@ -475,16 +519,14 @@ __global__ __launch_bounds__(ATT_THREADS, WIDE ? 2 : 1) void attend_kernel(Atten
         const char *kl = mine + ((i + 1) & 1) * STAGE, *vl = mine + 2 * STAGE + (i & 1) * STAGE;
         copies_done();
         __syncthreads();  // K of block i + 1 and V of block i are there, and nobody reads the ones before any more
-        if (i + 1 < steps) {
-          if ((i + 1) % PER == 0) v_at = k_at;
-          copy(v_at, i + 1, vb, false);
-        }
+        if (i + 1 < steps) copy_v(rows, i + 1);
         if (i + 2 < steps) {
           if ((i + 2) % PER == 0) {
-            k_at = stretch((i + 2) / PER, next);
+            at = stretch((i + 2) / PER, next);
             next = ask((i + 2) / PER + 1);
           }
-          copy(k_at, i + 2, kb, true);
+          rows = groups(at, i + 2);
+          copy_k(rows, i + 2);
         }
         if (!live) return;
         const int k0 = begin + i * STEP;
@@ -502,18 +544,19 @@ __global__ __launch_bounds__(ATT_THREADS, WIDE ? 2 : 1) void attend_kernel(Atten
         if (i + 1 < steps) step(i + 1, s1, s0);
       }
     } else {
-      copy(k_at, 0, kb, true);
-      copy(k_at, 0, vb, false);
+      copy_k(rows, 0);
+      copy_v(rows, 0);
       int32_t next = ask(1);
       for (int i = 0; i < steps; ++i) {
         copies_done();
         if (i + 1 < steps) {
           if ((i + 1) % PER == 0) {
-            k_at = stretch((i + 1) / PER, next);
+            at = stretch((i + 1) / PER, next);
             next = ask((i + 1) / PER + 1);
           }
-          copy(k_at, i + 1, kb, true);
-          copy(k_at, i + 1, vb, false);
+          rows = groups(at, i + 1);
+          copy_k(rows, i + 1);
+          copy_v(rows, i + 1);
         }
         const int k0 = begin + i * STEP + 32 * wave, k1 = k0 + 31;
         if (k0 > wave_hi || k1 < wave_lo) continue;
