@@ -335,7 +335,7 @@ struct PhaseSums {
 // of the batch do not fill the chip (two work-groups of 128 rows a compute unit), keys are split so that they do, in
 // stretches that pay for their partial results.
 static void shape_phase(const PhaseSums& s, int Hkv, int tile, AttendPhase* ph) {
-  ph->tile = tile;
+  ph->log2_tile = tile == 128 ? 7 : 5;
   const int64_t base = s.tiles * Hkv;
   double chunk = (double)s.max_keys + 64;
   if (base > 0 && base < 512) chunk = std::max(s.keys * Hkv / 512, tile == 128 ? 512.0 : 256.0);
@@ -419,8 +419,7 @@ static int plan_attend(const absb_layer* layer, const absb_batch* batch, const a
     }
   }
   p.parts = p.shared.splits + p.own.splits;
-  for (const AttendPhase* ph : {&p.shared, &p.own})
-    if (ph->slots * Hkv * ph->splits >= (int64_t(1) << 31)) return ABSB_ERR_BAD_SHAPE;
+  if (p.shared.slots * Hkv * p.shared.splits + p.own.slots * Hkv * p.own.splits >= (int64_t(1) << 31)) return ABSB_ERR_BAD_SHAPE;
   const int64_t pairs = p.rows * layer->num_q_heads;
   if (ceil_div(pairs, 4) >= (int64_t(1) << 31)) return ABSB_ERR_BAD_SHAPE;
   if (p.parts > 1 && p.rows) {
@@ -849,6 +848,9 @@ static int attend(const absb_layer* layer, const absb_batch* batch, const absb_r
   p.G = p.Hq / p.Hkv;
   p.log2_page = ilog2(layer->page_size);
   p.parts = plan.parts;
+  p.shared = plan.shared;
+  p.own = plan.own;
+  p.shared_units = (uint32_t)(plan.shared.slots * p.Hkv * plan.shared.splits);
   const float scale = resolve_scale(layer);
   p.scale_log2 = scale * 1.4426950408889634f;
   if (cap > 0.0f) {

@@ -10,7 +10,7 @@ namespace absb {
 // and can be searched without a list; a slot without rows leaves at once.
 struct AttendPhase {
   int32_t owners;
-  int32_t tile;    // rows (token, query head of the group) of a work-group: 128, or 32 that its four waves share
+  int32_t log2_tile;  // rows (token, query head of the group) of a work-group: 128, or 32 that its four waves share
   int32_t splits;  // of a tile's keys, a work-group each
   int32_t chunk;   // keys of a split, a multiple of 128
   int64_t slots;   // tiles, empty ones included
@@ -36,11 +36,12 @@ struct AttendParams {
   float* part_ml;  // [rows][Hq][parts][2]: maximum in log2 units, sum
   int64_t s_page, s_head, s_tok;  // bytes
   int32_t batch, groups, pt_stride, Hq, Hkv, G, log2_page;
-  int32_t window, parts, part0;   // part0: of this phase's first split
+  int32_t window, parts;
   float scale_log2;               // sm_scale * log2(e)
   float cap_log2, cap_in;         // cap * log2(e), 2 log2(e) sm_scale / cap (capped only)
   int32_t cap_wide;               // 1: the cap is so far above ordinary scores that small ones need the series
-  AttendPhase phase;
+  uint32_t shared_units;          // work-groups of the first phase, ahead of the second's
+  AttendPhase shared, own;
 };
 
 ABSB_HIDDEN int launch_attend(const AttendParams& p, const AttendPlan& plan, int dtype, bool capped, hipStream_t stream);

@@ -58,18 +58,37 @@ __device__ __forceinline__ float across_halves(float x, Op op) {
   return op(bitcast<float>(h[0]), bitcast<float>(h[1]));
 }
 
-// Largest o in [0, n) with slot0(o) <= x, slot0 increasing, slot0(0) <= x; the wave looks at 64 places at a time.
+// The owner of tile slot x: the largest o in [0, n) with slot0(o) <= x, where slot0(o) = row0(o) * G / tile + o, and its rows
+// [row0(o), row0(o + 1)).  The wave looks at 64 places at a time; up to 63 owners are one look.
+struct Owner {
+  int o, r0, r1;
+};
 template <typename F>
-__device__ __forceinline__ int last_at_most(int n, int64_t x, F slot0) {
-  int lo = 0, hi = n;
+__device__ __forceinline__ Owner owner_of(int n, int64_t x, int G, int log2_tile, F row0) {
   const int lane = threadIdx.x & 63;
-  while (hi - lo > 1) {
+  int lo = 0, hi = n;  // the owner is in [lo, hi)
+  while (hi - lo > 63) {
     const int step = (hi - lo + 63) >> 6, at = lo + lane * step;
-    const uint64_t below = __ballot(at < hi && slot0(min(at, hi - 1)) <= x);
+    const uint64_t below = __ballot(at < hi && (((int64_t)row0(min(at, hi - 1)) * G) >> log2_tile) + at <= x);
     lo += (__popcll(below) - 1) * step;
     hi = min(hi, lo + step);
   }
-  return lo;
+  const int at = min(lo + lane, hi), r = row0(at);
+  const uint64_t below = __ballot(lo + lane < hi && (((int64_t)r * G) >> log2_tile) + at <= x);
+  const int i = __popcll(below) - 1;
+  return Owner{lo + i, __builtin_amdgcn_readlane(r, i), __builtin_amdgcn_readlane(r, i + 1)};
+}
+// The shared tokens of request b: those of the last group g with first[g] <= b.
+__device__ __forceinline__ int shared_tokens(const AttendParams& p, int b) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, hi = p.groups;
+  while (hi - lo > 64) {
+    const int step = (hi - lo + 63) >> 6, at = lo + lane * step;
+    lo += (__popcll(__ballot(at < hi && p.first[min(at, hi - 1)] <= b)) - 1) * step;
+    hi = min(hi, lo + step);
+  }
+  const int at = min(lo + lane, hi - 1), len = p.len[at];
+  return __builtin_amdgcn_readlane(len, __popcll(__ballot(lo + lane < hi && p.first[at] <= b)) - 1);
 }
 
 struct RowOf {
@@ -329,20 +348,25 @@ __device__ __forceinline__ LaneCopy lane_copy(uint32_t pitch) {
   for (int i = 0; i < 2; ++i) c.value[i] = (4 * i + r4) * pitch + ((piece ^ (r4 << 2)) * 16);
   return c;
 }
-// Copies N groups of eight rows, at `off` of K or V, to LDS.  `most`: the last row of each group that exists (`full`: all do); the
-// ones behind it are that row again, which no one sees.
+// N times eight rows of a block: where they start, the last of each that exists, and whether all do.
+template <int N>
+struct Groups {
+  uint64_t off[N];
+  int most[N];
+  bool full;
+};
+// Copies them from K or V to LDS, 2 N copies; rows that do not exist are the last that does again, which no one sees.
 template <bool KEY, int N>
-__device__ __forceinline__ void copy_groups(const char* base, const uint64_t (&off)[N], const int (&most)[N], bool full, uint32_t pitch,
-                                            const LaneCopy& lc, uint32_t to) {
+__device__ __forceinline__ void copy_groups(const char* base, const Groups<N>& g, uint32_t pitch, const LaneCopy& lc, uint32_t to) {
   auto copy = [&](auto all) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < 2 * N; ++j) {
       uint32_t at = KEY ? lc.key[j & 3] : lc.value[j & 1];
-      if (!decltype(all)::value) at -= (uint32_t)max(0, 4 * (j & 1) + (int)((threadIdx.x & 63) >> 4) - most[j >> 1]) * pitch;
-      copy_to_lds(base + off[j >> 1], at, to + 4 * j * ROW_BYTES);
+      if (!decltype(all)::value) at -= (uint32_t)max(0, 4 * (j & 1) + (int)((threadIdx.x & 63) >> 4) - g.most[j >> 1]) * pitch;
+      copy_to_lds(base + g.off[j >> 1], at, to + 4 * j * ROW_BYTES);
     }
   };
-  if (full) {
+  if (g.full) {
     copy(std::true_type());
   } else {
     rarely();
@@ -352,10 +376,14 @@ __device__ __forceinline__ void copy_groups(const char* base, const uint64_t (&o
 
 // The wave's copies have arrived, and what it read of LDS has, too (the next copy may overwrite it).
 __device__ __forceinline__ void copies_done() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
+// All but the last N loads of the wave have arrived (they do in order).
+template <int N>
+__device__ __forceinline__ void copies_but() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+// What the wave read of LDS has arrived: a copy may take its place.
+__device__ __forceinline__ void lds_read() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
 // The interval of a row, and the row itself: pair f = f0 + i of the tile.
-template <bool SHARED>
-__device__ __forceinline__ RowOf row_of(const AttendParams& p, const Tile& t, int own_from, int group, int kv_head, int64_t f) {
+__device__ __forceinline__ RowOf row_of(const AttendParams& p, const Tile& t, bool shared, int own_from, int group, int kv_head, int64_t f) {
   RowOf r;
   r.row = -1;
   r.head = kv_head * p.G;
@@ -367,7 +395,7 @@ __device__ __forceinline__ RowOf row_of(const AttendParams& p, const Tile& t, in
   r.row = t.r0 + tok;
   r.head += g;
   int b = t.table_row;
-  if (SHARED) {
+  if (shared) {
     r.hi = t.limit - 1;
     if (p.window || p.slopes) {  // the request that the row belongs to
       int lo = p.first[group], hi = p.first[group + 1];
@@ -388,36 +416,39 @@ __device__ __forceinline__ RowOf row_of(const AttendParams& p, const Tile& t, in
   return r;
 }
 
-template <int DT, bool CAP, bool BIAS, bool SHARED, bool WIDE>
-__global__ __launch_bounds__(ATT_THREADS, WIDE ? 2 : 1) void attend_kernel(AttendParams p) {
-  constexpr int TILE = WIDE ? 128 : 32;
-  // WIDE: a block of 64 keys that all waves use, twice.  Otherwise: 32 keys a wave, twice, and later the waves' outputs.
-  constexpr int STAGE = WIDE ? 64 * ROW_BYTES : 32 * ROW_BYTES;  // of K, and of V
-  __shared__ __align__(16) char s_kv[WIDE ? 4 * STAGE : 4 * STAGE * ATT_WAVES];
+constexpr int ATT_LDS = 65536;  // wide: a block of 64 keys, twice; narrow: 32 keys a wave, and later the waves' outputs
+
+template <int DT, bool CAP, bool BIAS>
+__global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) {
+  __shared__ __align__(16) char s_kv[ATT_LDS];
+  __shared__ float s_ml[ATT_WAVES][2][32];
   __shared__ int s_lo[ATT_WAVES], s_hi[ATT_WAVES];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
 
-  // ---- which tile, KV head and split: heads go round the dies first, so that a head's keys stay in one die's L2 where there
-  // are eight; long tiles (the last of a causal prompt) start first
-  const uint32_t unit = blockIdx.x;
+  // ---- which phase, tile, KV head and split: heads go round the dies first, so that a head's keys stay in one die's L2 where
+  // there are eight; long tiles (prefixes, the last ones of a causal prompt) start first
+  const bool shared = blockIdx.x < p.shared_units;
+  const uint32_t unit = shared ? blockIdx.x : blockIdx.x - p.shared_units;
+  const AttendPhase& ph = shared ? p.shared : p.own;
+  const int owners = ph.owners, splits = ph.splits, log2_tile = ph.log2_tile, chunk = ph.chunk;
+  const int part0 = shared ? 0 : p.shared.splits;
+  const bool wide = log2_tile == 7;
   const int kv_head = (int)(unit % (uint32_t)p.Hkv);
   const uint32_t rest = unit / (uint32_t)p.Hkv;
-  const int split = (int)(rest % (uint32_t)p.phase.splits);
-  const int64_t slot = p.phase.slots - 1 - (int64_t)(rest / (uint32_t)p.phase.splits);
-  auto row0 = [&](int o) { return p.row_off[SHARED ? p.first[o] : o]; };
-  auto slot0 = [&](int o) { return (int64_t)row0(o) * p.G / TILE + o; };
-  const int owner = last_at_most(p.phase.owners, slot, slot0);
+  const int split = (int)(rest % (uint32_t)splits);
+  const int64_t slot = ph.slots - 1 - (int64_t)(rest / (uint32_t)splits);
+  const Owner own = owner_of(owners, slot, p.G, log2_tile, [&](int o) { return p.row_off[shared ? p.first[o] : o]; });
+  const int owner = own.o;
   Tile t;
-  t.r0 = row0(owner);
-  t.n = row0(owner + 1) - t.r0;
-  t.f0 = (slot - slot0(owner)) * TILE;
+  t.r0 = own.r0;
+  t.n = own.r1 - own.r0;
+  t.f0 = (slot - (((int64_t)t.r0 * p.G >> log2_tile) + owner)) << log2_tile;
   if (t.f0 >= (int64_t)t.n * p.G) return;
-  t.table_row = SHARED ? p.first[owner] : owner;
-  t.limit = SHARED ? p.len[owner] : p.seq_lens[owner];
-  int own_from = 0;
-  if (!SHARED && p.first) own_from = p.len[last_at_most(p.groups, owner, [&](int g) { return (int64_t)p.first[g]; })];
+  t.table_row = shared ? p.first[owner] : owner;
+  t.limit = shared ? p.len[owner] : p.seq_lens[owner];
+  const int own_from = !shared && p.groups ? shared_tokens(p, owner) : 0;
 
-  const RowOf row = row_of<SHARED>(p, t, own_from, owner, kv_head, t.f0 + (WIDE ? 32 * wave : 0) + (lane & 31));
+  const RowOf row = row_of(p, t, shared, own_from, owner, kv_head, t.f0 + (wide ? 32 * wave : 0) + (lane & 31));
   const bool valid = row.row >= 0, sees = valid && row.lo <= row.hi;
   const int lo = sees ? row.lo : INT32_MAX, hi = sees ? row.hi : -1;
   auto lesser = [](uint32_t a, uint32_t b) { return a < b ? a : b; };
@@ -427,7 +458,7 @@ __global__ __launch_bounds__(ATT_THREADS, WIDE ? 2 : 1) void attend_kernel(Atten
   const int all_lo = (int)wave_reduce_u32((uint32_t)(valid ? row.lo : 0), greater);
   const int all_hi = (int)wave_reduce_u32((uint32_t)((valid ? row.hi : INT32_MAX - 1) + 1), lesser) - 1;
   int tile_lo = wave_lo, tile_hi = wave_hi;
-  if (WIDE) {
+  if (wide) {
     if (lane == 0) {
       s_lo[wave] = wave_lo;
       s_hi[wave] = wave_hi;
@@ -445,9 +476,9 @@ __global__ __launch_bounds__(ATT_THREADS, WIDE ? 2 : 1) void attend_kernel(Atten
     for (int j = 0; j < 16; ++j) st.o[i][j] = 0.0f;
 
   // ---- the split's keys [begin, end)
-  const int64_t from = ((int64_t)tile_lo & ~int64_t(63)) + (int64_t)split * p.phase.chunk;
+  const int64_t from = ((int64_t)tile_lo & ~int64_t(63)) + (int64_t)split * chunk;
   const int begin = (int)min(from, (int64_t)tile_hi + 1);
-  const int end = (int)min(from + p.phase.chunk, (int64_t)tile_hi + 1);
+  const int end = (int)min(from + chunk, (int64_t)tile_hi + 1);
   if (begin < end) {
     u32x4 q[8];
 #pragma unroll
@@ -459,54 +490,41 @@ __global__ __launch_bounds__(ATT_THREADS, WIDE ? 2 : 1) void attend_kernel(Atten
     const int32_t* pages = p.page_table + (int64_t)t.table_row * p.pt_stride;
     const char *kb = p.k + kv_head * p.s_head, *vb = p.v + kv_head * p.s_head;
     constexpr bool SCALED = CAP || BIAS;
-    constexpr int STEP = WIDE ? 64 : 128;  // keys of a step; narrow: 32 a wave
-    constexpr int PER = 512 / STEP;        // steps of a stretch
-    const int steps = (end - begin + STEP - 1) / STEP;
-    const char* mine = WIDE ? s_kv : s_kv + wave * 4 * STAGE;
-    const uint32_t mine_lds = lds_address(mine);
     auto stretch_begin = [&](int n) { return (int)min((int64_t)begin + (int64_t)n * 512, (int64_t)t.limit - 1); };
     auto ask = [&](int n) { return ask_page(p, pages, stretch_begin(n), t.limit); };
     auto stretch = [&](int n, int32_t page) { return stretch_on(p, page, stretch_begin(n), t.limit); };
     const uint32_t pitch = (uint32_t)p.s_tok;  // (seven rows of at most 2^29 bytes)
     const LaneCopy lc = lane_copy(pitch);
-    constexpr int GROUPS = WIDE ? 2 : 4;  // of eight rows, that a wave copies of a block
-    struct Groups {
-      uint64_t off[GROUPS];
-      int most[GROUPS];
-      bool full;
-    };
-    // This wave's rows of step i, from the stretch that it is in.
-    auto groups = [&](const Stretch& s, int i) __attribute__((always_inline)) {
-      Groups g;
+    // This wave's N groups of eight rows of a block: from lane `from` of the stretch on.
+    auto groups = [&](const Stretch& s, int from, auto n) __attribute__((always_inline)) {
+      Groups<decltype(n)::value> g;
       g.full = true;
 #pragma unroll
-      for (int j = 0; j < GROUPS; ++j) {
-        const int from = WIDE ? (i % PER) * 8 + 2 * wave + j : (i % PER) * 16 + 4 * wave + j;
-        g.off[j] = lane_u64(s.off, from);
-        g.most[j] = __builtin_amdgcn_readlane(s.most, from);
+      for (int j = 0; j < decltype(n)::value; ++j) {
+        g.off[j] = lane_u64(s.off, from + j);
+        g.most[j] = __builtin_amdgcn_readlane(s.most, from + j);
         g.full = g.full && g.most[j] == 7;
       }
       return g;
     };
-    // Its K, or V, to buffer i % 2 (of K's two, or V's behind them).
-    const uint32_t to = mine_lds + (WIDE ? 16 * wave * ROW_BYTES : 0);
-    auto copy_k = [&](const Groups& g, int i) __attribute__((always_inline)) {
-      copy_groups<true, GROUPS>(kb, g.off, g.most, g.full, pitch, lc, to + (i & 1) * STAGE);
-    };
-    auto copy_v = [&](const Groups& g, int i) __attribute__((always_inline)) {
-      copy_groups<false, GROUPS>(vb, g.off, g.most, g.full, pitch, lc, to + (2 + (i & 1)) * STAGE);
-    };
     Stretch at = stretch(0, ask(0));
-    Groups rows = groups(at, 0);
-    if (WIDE) {
+    int32_t next = ask(1);
+    if (wide) {
+      constexpr int STEP = 64, PER = 512 / STEP, STAGE = STEP * ROW_BYTES;
+      const int steps = (end - begin + STEP - 1) / STEP;
+      const char* mine = s_kv;
+      const uint32_t to = lds_address(s_kv) + 16 * wave * ROW_BYTES;
+      auto copy_k = [&](const Groups<2>& g, int i) __attribute__((always_inline)) { copy_groups<true>(kb, g, pitch, lc, to + (i & 1) * STAGE); };
+      auto copy_v = [&](const Groups<2>& g, int i) __attribute__((always_inline)) { copy_groups<false>(vb, g, pitch, lc, to + (2 + (i & 1)) * STAGE); };
+      auto rows_of = [&](int i) __attribute__((always_inline)) { return groups(at, (i % PER) * 8 + 2 * wave, std::integral_constant<int, 2>()); };
+      Groups<2> rows = rows_of(0);
       // Step i: the scores of block i + 1 are worked out beside the softmax of block i, matrix and vector unit at once; so K is
       // copied two blocks ahead, V one.  (The last step works out scores of whatever is in LDS, for nobody.)
       copy_k(rows, 0);
       copy_v(rows, 0);
-      int32_t next = ask(1);
       copies_done();
       __syncthreads();
-      rows = groups(at, 1);
+      rows = rows_of(1);
       if (steps > 1) copy_k(rows, 1);
       const bool live = wave_lo <= wave_hi;  // (waves whose rows see nothing only copy)
       f32x16 s0[2], s1[2];
@@ -525,7 +543,7 @@ __global__ __launch_bounds__(ATT_THREADS, WIDE ? 2 : 1) void attend_kernel(Atten
             at = stretch((i + 2) / PER, next);
             next = ask((i + 2) / PER + 1);
           }
-          rows = groups(at, i + 2);
+          rows = rows_of(i + 2);
           copy_k(rows, i + 2);
         }
         if (!live) return;
@@ -544,43 +562,58 @@ __global__ __launch_bounds__(ATT_THREADS, WIDE ? 2 : 1) void attend_kernel(Atten
         if (i + 1 < steps) step(i + 1, s1, s0);
       }
     } else {
-      copy_k(rows, 0);
-      copy_v(rows, 0);
-      int32_t next = ask(1);
+      // Every wave by itself, 32 keys a step: K's buffer takes the next block's as soon as the scores have been worked out, V's as
+      // soon as the output has, so that copies are in flight all the time and no two waves wait for each other.
+      constexpr int STEP = 128, PER = 512 / STEP;
+      const int steps = (end - begin + STEP - 1) / STEP;
+      const char *kl = s_kv + wave * 64 * ROW_BYTES, *vl = kl + 32 * ROW_BYTES;
+      const uint32_t k_to = lds_address(kl), v_to = lds_address(vl);
+      auto rows_of = [&](int i) __attribute__((always_inline)) { return groups(at, (i % PER) * 16 + 4 * wave, std::integral_constant<int, 4>()); };
+      Groups<4> rows = rows_of(0);
+      copy_groups<true>(kb, rows, pitch, lc, k_to);
+      copy_groups<false>(vb, rows, pitch, lc, v_to);
       for (int i = 0; i < steps; ++i) {
-        copies_done();
-        if (i + 1 < steps) {
+        const int k0 = begin + i * STEP + 32 * wave, k1 = k0 + 31;
+        const bool live = k0 <= wave_hi && k1 >= wave_lo, more = i + 1 < steps;
+        f32x16 s[1];
+        copies_but<8>();  // K is there (behind it: V's eight copies)
+        if (live) s[0] = scores_of<DT>(kl, q);
+        lds_read();
+        if (more) {
           if ((i + 1) % PER == 0) {
             at = stretch((i + 1) / PER, next);
             next = ask((i + 1) / PER + 1);
           }
-          rows = groups(at, i + 1);
-          copy_k(rows, i + 1);
-          copy_v(rows, i + 1);
+          rows = rows_of(i + 1);
+          copy_groups<true>(kb, rows, pitch, lc, k_to);
         }
-        const int k0 = begin + i * STEP + 32 * wave, k1 = k0 + 31;
-        if (k0 > wave_hi || k1 < wave_lo) continue;
-        // (a split ends on a block or with the tile's last key, so what a row sees of a block is in its interval)
-        f32x16 s[1] = {scores_of<DT>(mine + (i & 1) * STAGE, q)};
-        adjust<CAP, BIAS, 1>(p, s, k0, k0 < all_lo || k1 > all_hi, row, slope_log2);
-        const float base = new_maximum<SCALED>(p, largest<1>(s), st);
         u32x4 w[2];
-        weigh<DT, SCALED, 1>(p, s, base, w, st);
-        add_values<DT, 1>(mine + 2 * STAGE + (i & 1) * STAGE, w, st);
+        if (live) {
+          // (a split ends on a block or with the tile's last key, so what a row sees of a block is in its interval)
+          adjust<CAP, BIAS, 1>(p, s, k0, k0 < all_lo || k1 > all_hi, row, slope_log2);
+          const float base = new_maximum<SCALED>(p, largest<1>(s), st);
+          weigh<DT, SCALED, 1>(p, s, base, w, st);
+        }
+        if (more)
+          copies_but<8>();  // V is there (behind it: the next K's eight)
+        else
+          copies_done();
+        if (live) add_values<DT, 1>(vl, w, st);
+        lds_read();
+        if (more) copy_groups<false>(vb, rows, pitch, lc, v_to);
       }
     }
   }
   st.l = across_halves(st.l, [](float a, float b) { return a + b; });
 
-  // ---- the waves of a narrow tile have keys of their own: their states become one, wave w's quarter of the channels of all
-  if (!WIDE) {
+  // ---- the waves of a narrow tile have keys of their own: their states become one, a quarter of the channels a wave
+  if (!wide) {
     __syncthreads();
-    float* s_o = reinterpret_cast<float*>(s_kv);             // [wave][channel][row], 16 KB a wave
-    float* s_ml = reinterpret_cast<float*>(s_kv + 65536);    // [wave][2][32]
+    float* s_o = reinterpret_cast<float*>(s_kv);  // [wave][channel][row]
     const int half = lane >> 5, col = lane & 31;
     if (half == 0) {
-      s_ml[wave * 64 + col] = st.m;
-      s_ml[wave * 64 + 32 + col] = st.l;
+      s_ml[wave][0][col] = st.m;
+      s_ml[wave][1][col] = st.l;
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -589,13 +622,13 @@ __global__ __launch_bounds__(ATT_THREADS, WIDE ? 2 : 1) void attend_kernel(Atten
     __syncthreads();
     float m = -__builtin_inff(), w[ATT_WAVES];
 #pragma unroll
-    for (int x = 0; x < ATT_WAVES; ++x) m = fmaxf(m, s_ml[x * 64 + col]);
+    for (int x = 0; x < ATT_WAVES; ++x) m = fmaxf(m, s_ml[x][0][col]);
     const float base = m == -__builtin_inff() ? 0.0f : m;
     float l = 0.0f;
 #pragma unroll
     for (int x = 0; x < ATT_WAVES; ++x) {
-      w[x] = exp2_fast(s_ml[x * 64 + col] - base);
-      l = __builtin_fmaf(s_ml[x * 64 + 32 + col], w[x], l);
+      w[x] = exp2_fast(s_ml[x][0][col] - base);
+      l = __builtin_fmaf(s_ml[x][1][col], w[x], l);
     }
     st.m = m;
     st.l = l;
@@ -610,105 +643,99 @@ __global__ __launch_bounds__(ATT_THREADS, WIDE ? 2 : 1) void attend_kernel(Atten
   }
   if (!valid) return;
 
-  // ---- out: channels 32 t + 8 (i / 4) + 4 half + i % 4, four at a time
+  // ---- out: channels 32 t + 8 (i / 4) + 4 half + i % 4, four at a time (narrow: the wave's 32, in o[0])
   const int half = lane >> 5;
   const int64_t at = (int64_t)row.row * p.Hq + row.head;
-  const bool writes_ml = half == 0 && (WIDE || wave == 0);
-  constexpr int TILES = WIDE ? 4 : 1;
-  if (p.parts == 1) {
-    const float inv = st.l > 0.0f ? 1.0f / st.l : 0.0f;
-#pragma unroll
-    for (int i = 0; i < TILES; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int ch = 32 * (WIDE ? i : wave) + 8 * j + 4 * half;
-        const uint2 w = {pack2<DT>(st.o[i][4 * j] * inv, st.o[i][4 * j + 1] * inv), pack2<DT>(st.o[i][4 * j + 2] * inv, st.o[i][4 * j + 3] * inv)};
-        *reinterpret_cast<uint2*>(p.out + at * ABSB_HEAD_DIM + ch) = w;
-      }
-    if (writes_ml && p.lse) p.lse[at] = st.l > 0.0f ? (st.m + __builtin_log2f(st.l)) * LN2 : -__builtin_inff();
-    return;
+  const bool one = p.parts == 1;
+  const int64_t part = at * p.parts + part0 + split;
+  const float inv = st.l > 0.0f ? 1.0f / st.l : 0.0f;
+  if (half == 0 && (wide || wave == 0)) {
+    if (!one)
+      *reinterpret_cast<float2*>(p.part_ml + part * 2) = make_float2(st.m, st.l);
+    else if (p.lse)
+      p.lse[at] = st.l > 0.0f ? (st.m + __builtin_log2f(st.l)) * LN2 : -__builtin_inff();
   }
-  const int64_t part = at * p.parts + p.part0 + split;
-  if (writes_ml) *reinterpret_cast<float2*>(p.part_ml + part * 2) = make_float2(st.m, st.l);
-  if (begin < end) {  // (a split without keys has weight 0: its sum says so)
+  if (!one && begin >= end) return;  // (a split without keys has weight 0: its sum says so)
+  auto put = [&](int ch, float a, float b, float c, float d) __attribute__((always_inline)) {
+    if (one) {
+      const uint2 w = {pack2<DT>(a * inv, b * inv), pack2<DT>(c * inv, d * inv)};
+      *reinterpret_cast<uint2*>(p.out + at * ABSB_HEAD_DIM + ch) = w;
+    } else {
+      *reinterpret_cast<f32x4*>(p.part_o + part * ABSB_HEAD_DIM + ch) = f32x4{a, b, c, d};
+    }
+  };
 #pragma unroll
-    for (int i = 0; i < TILES; ++i)
+  for (int i = 0; i < 4; ++i) {
+    if (!wide && i > 0) break;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int ch = 32 * (WIDE ? i : wave) + 8 * j + 4 * half;
-        *reinterpret_cast<f32x4*>(p.part_o + part * ABSB_HEAD_DIM + ch) = f32x4{st.o[i][4 * j], st.o[i][4 * j + 1], st.o[i][4 * j + 2], st.o[i][4 * j + 3]};
-      }
+    for (int j = 0; j < 4; ++j)
+      put(32 * (wide ? i : wave) + 8 * j + 4 * half, st.o[i][4 * j], st.o[i][4 * j + 1], st.o[i][4 * j + 2], st.o[i][4 * j + 3]);
   }
 }
 
-// The parts of a (row, query head), a wave each: a lane has two channels.
+// The parts of a (row, query head), a wave each: half a wave a part, a lane four channels.
 template <int DT>
 __global__ __launch_bounds__(256) void attend_merge_kernel(AttendParams p, int64_t pairs) {
   const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (at >= pairs) return;
-  const int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63, half = lane >> 5;
   const float* ml = p.part_ml + at * p.parts * 2;
-  const float* o = p.part_o + at * p.parts * ABSB_HEAD_DIM + 2 * lane;
-  float M = -__builtin_inff(), L = 0.0f, x = 0.0f, y = 0.0f;
+  const float* o = p.part_o + at * p.parts * ABSB_HEAD_DIM + 4 * (lane & 31);
+  constexpr int TRIP = 8;  // parts fetched at once
+  float M = -__builtin_inff(), L = 0.0f;
+  f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
   for (int i0 = 0; i0 < p.parts; i0 += 64) {
     float2 mine = make_float2(-__builtin_inff(), 0.0f);
     if (i0 + lane < p.parts) mine = *reinterpret_cast<const float2*>(ml + (i0 + lane) * 2);
-    if (!(mine.y > 0.0f)) mine.x = -__builtin_inff();
+    if (!(mine.y > 0.0f)) mine = make_float2(-__builtin_inff(), 0.0f);
     const float top = fmaxf(M, wave_max_f32(mine.x)), base = top == -__builtin_inff() ? 0.0f : top;
     const float a = exp2_fast(M - base), w = exp2_fast(mine.x - base);
     M = top;
-    L *= a;
+    L = __builtin_fmaf(L, a, mine.y * w);  // (a lane's own parts)
     x *= a;
-    y *= a;
     const int n = min(64, p.parts - i0);
-    for (int i = 0; i < n; ++i) {
-      const float wi = bitcast<float>(__builtin_amdgcn_readlane(bitcast<int>(w), i));
-      if (wi == 0.0f) continue;  // (its output may never have been written)
-      const float li = bitcast<float>(__builtin_amdgcn_readlane(bitcast<int>(mine.y), i));
-      const float2 v = *reinterpret_cast<const float2*>(o + (int64_t)(i0 + i) * ABSB_HEAD_DIM);
-      L = __builtin_fmaf(li, wi, L);
-      x = __builtin_fmaf(v.x, wi, x);
-      y = __builtin_fmaf(v.y, wi, y);
+    for (int i = 0; i < n; i += TRIP) {
+      f32x4 v[TRIP / 2];
+#pragma unroll
+      for (int j = 0; j < TRIP / 2; ++j)
+        v[j] = *reinterpret_cast<const f32x4*>(o + (int64_t)(i0 + min(i + 2 * j + half, n - 1)) * ABSB_HEAD_DIM);
+#pragma unroll
+      for (int j = 0; j < TRIP / 2; ++j) {
+        const float wi = __shfl(w, min(i + 2 * j + half, 63));
+        if (i + 2 * j + half < n && wi != 0.0f) x += v[j] * wi;  // (an output of weight 0 may never have been written)
+      }
     }
   }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x[j] = across_halves(x[j], [](float a, float b) { return a + b; });
+  L = row16_sum(L);
+  L = bitcast<float>(__builtin_amdgcn_readlane(bitcast<int>(L), 0)) + bitcast<float>(__builtin_amdgcn_readlane(bitcast<int>(L), 16)) +
+      bitcast<float>(__builtin_amdgcn_readlane(bitcast<int>(L), 32)) + bitcast<float>(__builtin_amdgcn_readlane(bitcast<int>(L), 48));
   const float inv = L > 0.0f ? 1.0f / L : 0.0f;
-  *reinterpret_cast<uint32_t*>(p.out + at * ABSB_HEAD_DIM + 2 * lane) = pack2<DT>(x * inv, y * inv);
+  if (half == 0)
+    *reinterpret_cast<uint2*>(p.out + at * ABSB_HEAD_DIM + 4 * lane) = uint2{pack2<DT>(x[0] * inv, x[1] * inv), pack2<DT>(x[2] * inv, x[3] * inv)};
   if (p.lse && lane == 0) p.lse[at] = L > 0.0f ? (M + __builtin_log2f(L)) * LN2 : -__builtin_inff();
 }
 
-template <int DT, bool CAP, bool BIAS, bool SHARED>
-static void launch_tiles(const AttendParams& p, dim3 grid, hipStream_t stream) {
-  if (p.phase.tile == 128)
-    hipLaunchKernelGGL((attend_kernel<DT, CAP, BIAS, SHARED, true>), grid, dim3(ATT_THREADS), 0, stream, p);
-  else
-    hipLaunchKernelGGL((attend_kernel<DT, CAP, BIAS, SHARED, false>), grid, dim3(ATT_THREADS), 0, stream, p);
-}
 template <int DT, bool CAP, bool BIAS>
-static void launch_phases(AttendParams p, const AttendPlan& plan, hipStream_t stream) {
-  auto grid = [&](const AttendPhase& ph) { return dim3((unsigned)(ph.slots * p.Hkv * ph.splits)); };
-  if (plan.shared.owners) {
-    p.phase = plan.shared;
-    p.part0 = 0;
-    launch_tiles<DT, CAP, BIAS, true>(p, grid(p.phase), stream);
-  }
-  p.phase = plan.own;
-  p.part0 = plan.parts - plan.own.splits;
-  launch_tiles<DT, CAP, BIAS, false>(p, grid(p.phase), stream);
-  if (plan.parts > 1) {
-    const int64_t pairs = plan.rows * p.Hq;
+static void launch_parts(const AttendParams& p, int64_t rows, hipStream_t stream) {
+  const int64_t own_units = p.own.slots * p.Hkv * p.own.splits;
+  hipLaunchKernelGGL((attend_kernel<DT, CAP, BIAS>), dim3((unsigned)(p.shared_units + own_units)), dim3(ATT_THREADS), 0, stream, p);
+  if (p.parts > 1) {
+    const int64_t pairs = rows * p.Hq;
     hipLaunchKernelGGL((attend_merge_kernel<DT>), dim3((unsigned)((pairs + 3) / 4)), dim3(256), 0, stream, p, pairs);
   }
 }
 template <int DT>
 static void launch_typed(const AttendParams& p, const AttendPlan& plan, bool capped, hipStream_t stream) {
   if (capped && p.slopes)
-    launch_phases<DT, true, true>(p, plan, stream);
+    launch_parts<DT, true, true>(p, plan.rows, stream);
   else if (capped)
-    launch_phases<DT, true, false>(p, plan, stream);
+    launch_parts<DT, true, false>(p, plan.rows, stream);
   else if (p.slopes)
-    launch_phases<DT, false, true>(p, plan, stream);
+    launch_parts<DT, false, true>(p, plan.rows, stream);
   else
-    launch_phases<DT, false, false>(p, plan, stream);
+    launch_parts<DT, false, false>(p, plan.rows, stream);
 }
 
 int launch_attend(const AttendParams& p, const AttendPlan& plan, int dtype, bool capped, hipStream_t stream) {
