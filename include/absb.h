@@ -505,11 +505,12 @@ typedef struct absb_shared_prefix {
   const int32_t* len;           /* device [groups], same values                                  */
 } absb_shared_prefix;
 
-/* Workspace of the two entry points below for these rows and any options (`shared` NULL: of
- * absb_attend_rows).  May be 0.  Nothing in it needs initialisation or survives a call; calls that share one must
- * be ordered on one stream.  Reads host fields only. */
+/* Workspace of the two entry points below for these rows (`shared` NULL: of absb_attend_rows) and options; opts NULL:
+ * enough for whatever options.  May be 0.  Nothing in it needs initialisation or survives a call; calls that share one
+ * must be ordered on one stream.  Reads host fields only (of the options the window, and whether prefixes are set). */
 ABSB_API int absb_attend_workspace(const absb_layer* layer, const absb_batch* batch, const absb_rows* rows,
-                                   const absb_shared_prefix* shared, size_t* workspace_bytes);
+                                   const absb_shared_prefix* shared, const absb_score_opts* opts,
+                                   size_t* workspace_bytes);
 
 /* Dense attention of every request's rows over its context in the paged caches, the rows' own keys and
  * values included (absb_rotate_store has written them).  Prompts, chunks of prompts, single tokens, any

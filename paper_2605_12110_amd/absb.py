@@ -111,7 +111,7 @@ _ARGTYPES = {
     "absb_map_rows": [_REC, _REC, _P, _P, _REC, C.c_int32, _P, _P, _P, _P],
     "absb_rope_frequencies": [_REC, _P],
     "absb_rotate_store": [_REC, _REC, C.c_int32, _P, _P, _P, _P, C.c_int64, _P, _P, C.c_int64, _P, C.c_int64, _P, _P, _P],
-    "absb_attend_workspace": [_REC, _REC, _REC, _REC, _P],
+    "absb_attend_workspace": [_REC, _REC, _REC, _REC, _REC, _P],
     "absb_attend_rows": [_REC, _REC, _REC, _P, _P, _P, _P, _P, _REC, _P, C.c_size_t, _P],
     "absb_attend_shared": [_REC, _REC, _REC, _REC, _P, _P, _P, _P, _P, _REC, _P, C.c_size_t, _P],
 }
@@ -579,10 +579,11 @@ def absb_rotate_store(layer: Layer, rope: Rope, row_pos, row_slot, freq, q=None,
                                     _ptr(k), ks, _ptr(v), vs, _ptr(k_cache), _ptr(v_cache), _stream(stream)), where)
 
 
-def absb_attend_workspace(layer: Layer, batch: Batch, rows: Rows, shared: SharedPrefix = None) -> int:
+def absb_attend_workspace(layer: Layer, batch: Batch, rows: Rows, shared: SharedPrefix = None, opts: ScoreOpts = None) -> int:
+    """Bytes; without `opts`: enough for any options."""
     cl, cb = layer.c(), batch.c()
     n = C.c_size_t(0)
-    _check(load().absb_attend_workspace(C.byref(cl), C.byref(cb), _rec(rows), _rec(shared), C.byref(n)), "absb_attend_workspace")
+    _check(load().absb_attend_workspace(C.byref(cl), C.byref(cb), _rec(rows), _rec(shared), _rec(opts), C.byref(n)), "absb_attend_workspace")
     return int(n.value)
 
 

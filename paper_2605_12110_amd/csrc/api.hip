@@ -324,28 +324,60 @@ static int check_dense_layer(const absb_layer* layer) {
   return ABSB_OK;
 }
 
-// Owners of a phase, as the host sees them: rows (tokens), keys that a tile of theirs can see at most and on average.
+// The tiles of a phase, as the host sees them: how many (of a KV head), the keys of all of them together, of the longest, and of all
+// owners (read once, whatever the tiles).
 struct PhaseSums {
-  int64_t tiles = 0, max_rows = 0;
-  double keys = 0;  // over tiles: keys on average
-  int64_t max_keys = 0;
+  int64_t tiles = 0, max_keys = 0;
+  double keys = 0, owners_keys = 0;
 };
 
-// How a phase is cut.  The tile: 32 rows whose keys four waves share, if no owner has more, else 128.  Splits: while the tiles
-// of the batch do not fill the chip (two work-groups of 128 rows a compute unit), keys are split so that they do, in
-// stretches that pay for their partial results.
-static void shape_phase(const PhaseSums& s, int Hkv, int tile, AttendPhase* ph) {
-  ph->log2_tile = tile == 128 ? 7 : 5;
-  const int64_t base = s.tiles * Hkv;
-  double chunk = (double)s.max_keys + 64;
-  if (base > 0 && base < 512) chunk = std::max(s.keys * Hkv / 512, tile == 128 ? 512.0 : 256.0);
-  chunk = std::max(chunk, s.max_keys / 64.0);
-  ph->chunk = (int32_t)std::min<int64_t>(((int64_t)chunk + 127) / 128 * 128, int64_t(1) << 30);
-  ph->splits = (int32_t)std::max<int64_t>(1, ceil_div(s.max_keys + 63, ph->chunk));  // (a tile's keys start at a multiple of 64)
+// A phase whose longest tile is cut into that many stretches, or as few more as stretches of whole steps make.
+static AttendPhase cut_phase(const PhaseSums& s, int log2_tile, int64_t splits, int64_t owners, int64_t slots) {
+  AttendPhase ph = {};
+  if (s.max_keys == 0) return ph;
+  ph.owners = (int32_t)owners;
+  ph.slots = slots;
+  ph.log2_tile = log2_tile;
+  splits = std::min<int64_t>(std::max<int64_t>(splits, 1), 64);
+  ph.chunk = (int32_t)std::min<int64_t>(ceil_div(ceil_div(s.max_keys, splits), 128) * 128, int64_t(1) << 30);
+  ph.splits = (int32_t)ceil_div(s.max_keys, ph.chunk);
+  return ph;
+}
+
+// What a launch takes, in us; constants measured on shapes from one token behind 4 K to chunks of 512 behind 16 K, 64 requests behind
+// 32 K shared ones, 16 of 500 to 60000 tokens, each cut in 1 to 64 ways (within a quarter of the best there).
+//   128-row tiles are bound by the matrix unit: a key takes a work-group 0.018 us alone on a compute unit, twice that as one of two
+//   (512 work-groups in all).  Equal ones go in rounds; others leave part of one running behind, hardly any if they start
+//   in falling order, as a causal prompt's do.
+//   32-row tiles are bound by memory, 5.4 TB/s, or, if they are few, by what one work-group can ask for: 0.0093 us a key.
+//   The two share a launch well.  Partial results are written and read once; the merge is a launch of its own.
+static double attend_us(const PhaseSums (&s)[2], const AttendPhase (&ph)[2], double pairs, int Hkv) {
+  constexpr double PLACES = 512, KEY_ALONE = 0.018, KEY_PAIRED = 0.036, KEY_NARROW = 0.0093, BYTES_US = 5.4e6, START = 8, MERGE = 5;
+  const int parts = ph[0].splits + ph[1].splits;
+  double wide = 0, narrow = 0, bytes = 0, units = 0;
+  for (int i = 0; i < 2; ++i) {
+    if (!ph[i].owners) continue;
+    const bool equal = 20 * s[i].keys >= 19.0 * s[i].tiles * s[i].max_keys;
+    const double tiles = (double)s[i].tiles * Hkv, keys = s[i].keys * Hkv, longest = (double)std::min<int64_t>(ph[i].chunk, s[i].max_keys);
+    const double n = ph[i].splits == 1 ? tiles : equal ? tiles * ph[i].splits : std::max(tiles, keys / ph[i].chunk + 0.5 * tiles);
+    bytes += s[i].owners_keys * Hkv * 4 * ABSB_HEAD_DIM;
+    units += n;
+    if (ph[i].log2_tile == 7) {
+      const double key = KEY_ALONE + (KEY_PAIRED - KEY_ALONE) * std::min(1.0, n / PLACES);
+      const double behind = n <= PLACES ? 0.0 : ph[i].splits == 1 && 4 * s[i].keys < 3.0 * s[i].tiles * s[i].max_keys ? 0.1 : 0.4;
+      wide += equal ? std::ceil(n / PLACES) * longest * key : std::max(longest * key, keys * KEY_PAIRED / PLACES + behind * longest * KEY_PAIRED);
+    } else {
+      narrow += (equal ? 0.25 : 0.5) * longest * KEY_NARROW;
+      wide = std::max(wide, longest * KEY_NARROW);
+    }
+  }
+  narrow += bytes / BYTES_US;
+  const double merge = parts > 1 ? MERGE + parts / 16 + 2 * pairs * parts * (ABSB_HEAD_DIM + 2) * 4 / BYTES_US : 0.0;
+  return START + std::max(wide, narrow) + 0.35 * std::min(wide, narrow) + 2 * units / PLACES + merge;
 }
 
 static int plan_attend(const absb_layer* layer, const absb_batch* batch, const absb_rows* rows, const absb_shared_prefix* shared,
-                       const absb_score_opts* opts, AttendPlan* plan) {
+                       const absb_score_opts* opts, bool any_options, AttendPlan* plan) {
   int rc = check_dense_layer(layer);
   if (rc != ABSB_OK) return rc;
   if (!batch || !rows || !batch->seq_lens_host || !rows->row_off_host) return ABSB_ERR_NULL;
@@ -363,12 +395,12 @@ static int plan_attend(const absb_layer* layer, const absb_batch* batch, const a
   if ((int64_t)batch->pt_stride < ceil_div(max_len, P)) return ABSB_ERR_BAD_SHAPE;
   AttendPlan p = {};
   p.rows = off[Bt];
-  PhaseSums own, common;
-  const int own_tile = max_n * G <= 32 ? 32 : 128;
-  int shared_tile = 32;
+  PhaseSums sums[2];  // shared keys, own keys
+  // the tile: 32 rows whose keys four waves share, if no owner has more, else 128
+  int tile[2] = {5, max_n * G <= 32 ? 5 : 7};
   if (shared) {
     const int32_t* first = shared->first_host;
-    if (shared->groups < 1 || first[0] != 0 || first[shared->groups] != Bt) return ABSB_ERR_BAD_SHAPE;
+    if (shared->groups < 1 || first[0] != 0) return ABSB_ERR_BAD_SHAPE;
     int64_t most = 0;
     for (int g = 0; g < shared->groups; ++g) {
       if (first[g + 1] < first[g] || first[g + 1] > Bt) return ABSB_ERR_BAD_SHAPE;
@@ -378,53 +410,80 @@ static int plan_attend(const absb_layer* layer, const absb_batch* batch, const a
         if (lens[b] - (off[b + 1] - off[b]) < len) return ABSB_ERR_BAD_SHAPE;
       most = std::max<int64_t>(most, off[first[g + 1]] - off[first[g]]);
     }
-    shared_tile = most * G <= 32 ? 32 : 128;
+    if (first[shared->groups] != Bt) return ABSB_ERR_BAD_SHAPE;
+    if (most * G > 32) tile[0] = 7;
     for (int g = 0; g < shared->groups; ++g) {
-      const int64_t tiles = ceil_div((int64_t)(off[first[g + 1]] - off[first[g]]) * G, shared_tile);
-      common.tiles += tiles;
-      common.keys += (double)tiles * shared->len_host[g];
-      if (tiles) common.max_keys = std::max<int64_t>(common.max_keys, shared->len_host[g]);
+      const int64_t tiles = (((int64_t)(off[first[g + 1]] - off[first[g]]) * G - 1) >> tile[0]) + 1;
+      sums[0].tiles += tiles;
+      sums[0].keys += (double)tiles * shared->len_host[g];
+      if (tiles) sums[0].owners_keys += shared->len_host[g];
+      if (tiles) sums[0].max_keys = std::max<int64_t>(sums[0].max_keys, shared->len_host[g]);
     }
-    p.shared.owners = shared->groups;
-    p.shared.slots = (int64_t)off[Bt] * G / shared_tile + shared->groups;
-    shape_phase(common, Hkv, shared_tile, &p.shared);
-    if (common.max_keys == 0) p.shared = AttendPhase{};  // nobody shares anything
   }
-  const bool bounded = opts && opts->window && !opts->prefix_lens;  // no tile sees more keys than its window
+  // A tile starts at a multiple of 64 keys, which is up to 63 ahead of its own ones behind a prefix of small pages.
+  const bool early = shared && P < 64;
+  // No tile sees more keys than its window.  (With a shared prefix the cuts are made as if there were none.)
+  const bool bounded = opts && opts->window && !opts->prefix_lens && !shared;
   PhaseSums seen;
   int g = 0;
   for (int b = 0; b < Bt; ++b) {
     while (shared && b >= shared->first_host[g + 1]) ++g;
-    const int64_t n = off[b + 1] - off[b], tiles = ceil_div(n * G, own_tile);
+    const int64_t n = off[b + 1] - off[b], tiles = ((n * G - 1) >> tile[1]) + 1;
     if (!n) continue;
     const int64_t keys = lens[b] - (shared ? shared->len_host[g] : 0);
-    const int64_t most = bounded ? std::min<int64_t>(keys, (int64_t)opts->window + own_tile / G + 1) : keys;
     const double mean = keys - 0.5 * n;
-    own.tiles += tiles;
-    own.keys += mean * tiles;
-    own.max_keys = std::max(own.max_keys, keys);
-    seen.keys += std::min(mean, (double)most) * tiles;
-    seen.max_keys = std::max(seen.max_keys, most);
+    sums[1].tiles += tiles;
+    sums[1].keys += mean * tiles;
+    sums[1].owners_keys += keys;
+    sums[1].max_keys = std::max(sums[1].max_keys, keys + (early ? 63 : 0));
+    if (bounded) {
+      const int64_t most = std::min<int64_t>(keys, (int64_t)opts->window + (int64_t(1) << tile[1]) / G + 1);
+      seen.keys += std::min(mean, (double)most) * tiles;
+      seen.owners_keys += std::min<int64_t>(keys, opts->window + n);
+      seen.max_keys = std::max(seen.max_keys, most + 63);
+    }
   }
-  p.own.owners = Bt;
-  p.own.slots = (int64_t)off[Bt] * G / own_tile + Bt;
-  shape_phase(own, Hkv, own_tile, &p.own);
-  if (bounded) {  // never more splits than without the window: the workspace does not depend on the options
-    const int32_t splits = p.own.splits;
-    seen.tiles = own.tiles;
-    shape_phase(seen, Hkv, own_tile, &p.own);
-    if (p.own.splits > splits) {
-      p.own.chunk = (int32_t)(ceil_div(ceil_div(seen.max_keys + 63, splits), 128) * 128);
-      p.own.splits = (int32_t)ceil_div(seen.max_keys + 63, p.own.chunk);
+  seen.tiles = sums[1].tiles;
+  // Both phases' keys are cut into stretches that take about equally long (a narrow tile's key takes half of a wide one's).
+  const int64_t owners[2] = {shared ? shared->groups : 0, Bt};
+  const int64_t slots[2] = {(((int64_t)off[Bt] * G) >> tile[0]) + owners[0], (((int64_t)off[Bt] * G) >> tile[1]) + Bt};
+  auto choose = [&](const PhaseSums (&s)[2], int most_splits) {
+    double whole[2], best = 0;
+    for (int i = 0; i < 2; ++i) whole[i] = s[i].max_keys * (tile[i] == 7 ? 2.0 : 1.0);
+    for (int cuts = 1; cuts <= 64; cuts += cuts < 8 ? 1 : cuts < 16 ? 2 : 8) {
+      AttendPhase ph[2];
+      const double stretch = std::max(whole[0], whole[1]) / cuts;
+      for (int i = 0; i < 2; ++i) ph[i] = cut_phase(s[i], tile[i], (int64_t)std::ceil(whole[i] / stretch - 1e-6), owners[i], slots[i]);
+      if (ph[1].splits > most_splits) break;
+      const double us = attend_us(s, ph, (double)p.rows * layer->num_q_heads, Hkv);
+      if (cuts > 1 && us >= best) continue;
+      best = us;
+      p.shared = ph[0];
+      p.own = ph[1];
+    }
+  };
+  int parts_any = 0;  // the most that any options make
+  if (p.rows) {
+    choose(sums, 1 << 30);
+    parts_any = p.shared.splits + p.own.splits;
+    if (!shared) {
+      // a window may make more splits than there are without it, as many as fill the chip twice
+      const int64_t fill = ceil_div(1024, sums[1].tiles * Hkv);
+      parts_any = std::max(parts_any, (int)std::min<int64_t>(64, fill));
+    }
+    if (bounded) {
+      const PhaseSums windowed[2] = {PhaseSums{}, seen};
+      choose(windowed, parts_any);
     }
   }
   p.parts = p.shared.splits + p.own.splits;
+  const int ws_parts = any_options ? parts_any : p.parts;
   if (p.shared.slots * Hkv * p.shared.splits + p.own.slots * Hkv * p.own.splits >= (int64_t(1) << 31)) return ABSB_ERR_BAD_SHAPE;
   const int64_t pairs = p.rows * layer->num_q_heads;
   if (ceil_div(pairs, 4) >= (int64_t(1) << 31)) return ABSB_ERR_BAD_SHAPE;
-  if (p.parts > 1 && p.rows) {
-    p.ws_part_ml = align256((size_t)pairs * p.parts * ABSB_HEAD_DIM * 4);
-    p.ws_bytes = p.ws_part_ml + align256((size_t)pairs * p.parts * 2 * 4);
+  if (ws_parts > 1) {
+    p.ws_part_ml = align256((size_t)pairs * ws_parts * ABSB_HEAD_DIM * 4);
+    p.ws_bytes = p.ws_part_ml + align256((size_t)pairs * ws_parts * 2 * 4);
   }
   *plan = p;
   return ABSB_OK;
@@ -792,9 +851,10 @@ int absb_rotate_store(const absb_layer* layer, const absb_rope* rope, int32_t n_
 }
 
 int absb_attend_workspace(const absb_layer* layer, const absb_batch* batch, const absb_rows* rows,
-                          const absb_shared_prefix* shared, size_t* workspace_bytes) {
+                          const absb_shared_prefix* shared, const absb_score_opts* opts, size_t* workspace_bytes) {
+  if (opts && opts->window < 0) return ABSB_ERR_BAD_SHAPE;
   AttendPlan p;
-  int rc = plan_attend(layer, batch, rows, shared, nullptr, &p);
+  int rc = plan_attend(layer, batch, rows, shared, opts, !opts, &p);
   if (rc != ABSB_OK) return rc;
   if (!workspace_bytes) return ABSB_ERR_NULL;
   *workspace_bytes = p.ws_bytes;
@@ -804,11 +864,11 @@ int absb_attend_workspace(const absb_layer* layer, const absb_batch* batch, cons
 static int attend(const absb_layer* layer, const absb_batch* batch, const absb_rows* rows, const absb_shared_prefix* shared,
                   const void* q, const void* k_cache, const void* v_cache, void* out, float* lse,
                   const absb_score_opts* opts, void* workspace, size_t workspace_bytes, void* stream) {
-  AttendPlan plan;
-  int rc = plan_attend(layer, batch, rows, shared, opts, &plan);
-  if (rc != ABSB_OK) return rc;
   const float cap = opts ? opts->softcap : 0.0f;
   if (!(cap >= 0.0f) || std::isinf(cap) || (opts && opts->window < 0)) return ABSB_ERR_BAD_SHAPE;
+  AttendPlan plan;
+  int rc = plan_attend(layer, batch, rows, shared, opts, false, &plan);
+  if (rc != ABSB_OK) return rc;
   if (plan.rows == 0) return ABSB_OK;
   if (!q || !k_cache || !v_cache || !out || !batch->seq_lens || !batch->page_table || !rows->row_off) return ABSB_ERR_NULL;
   if (shared && (!shared->first || !shared->len)) return ABSB_ERR_NULL;

@@ -681,7 +681,7 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(AttendParams p, int64
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const float* ml = p.part_ml + at * p.parts * 2;
   const float* o = p.part_o + at * p.parts * ABSB_HEAD_DIM + 4 * (lane & 31);
-  constexpr int TRIP = 8;  // parts fetched at once
+  constexpr int TRIP = 16;  // parts fetched at once
   float M = -__builtin_inff(), L = 0.0f;
   f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
   for (int i0 = 0; i0 < p.parts; i0 += 64) {

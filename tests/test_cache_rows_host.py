@@ -202,10 +202,10 @@ def test_attend_refuses_null_records():
     lib = absb.load()
     cl, cb, cr = _layer().c(), _batch([5]).c(), _rows([1]).c()
     n = C.c_size_t(0)
-    assert lib.absb_attend_workspace(None, C.byref(cb), C.byref(cr), None, C.byref(n)) == absb.ERR_NULL
-    assert lib.absb_attend_workspace(C.byref(cl), None, C.byref(cr), None, C.byref(n)) == absb.ERR_NULL
-    assert lib.absb_attend_workspace(C.byref(cl), C.byref(cb), None, None, C.byref(n)) == absb.ERR_NULL
-    assert lib.absb_attend_workspace(C.byref(cl), C.byref(cb), C.byref(cr), None, None) == absb.ERR_NULL
+    assert lib.absb_attend_workspace(None, C.byref(cb), C.byref(cr), None, None, C.byref(n)) == absb.ERR_NULL
+    assert lib.absb_attend_workspace(C.byref(cl), None, C.byref(cr), None, None, C.byref(n)) == absb.ERR_NULL
+    assert lib.absb_attend_workspace(C.byref(cl), C.byref(cb), None, None, None, C.byref(n)) == absb.ERR_NULL
+    assert lib.absb_attend_workspace(C.byref(cl), C.byref(cb), C.byref(cr), None, None, None) == absb.ERR_NULL
     assert lib.absb_attend_shared(C.byref(cl), C.byref(cb), C.byref(cr), None, AT, AT, AT, AT, None, None, None, 0, None) == absb.ERR_NULL
 
 
@@ -222,4 +222,12 @@ def test_workspace_sizes(lens, new):
     size = absb.absb_attend_workspace(_layer(), _batch(lens), _rows(new))
     assert size % 256 == 0 and size <= sum(new) * 32 * 65 * 520 + 512
     shared = absb.SharedPrefix([0, len(lens)], [0], AT, AT)       # nothing shared: the same call
-    assert absb.absb_attend_workspace(_layer(), _batch(lens), _rows(new), shared) == size
+    plain = absb.ScoreOpts()
+    assert absb.absb_attend_workspace(_layer(), _batch(lens), _rows(new), shared, plain) == absb.absb_attend_workspace(
+        _layer(), _batch(lens), _rows(new), None, plain) <= size
+    # without options: enough for any window, and for prefixes
+    for opts in [absb.ScoreOpts(window=w) for w in (1, 17, 63, 64, 100, 129, 500, 1000, 2047, 4096, 10000, 100000, 2 ** 31 - 1)] + [
+            absb.ScoreOpts(window=100, prefix_lens=AT)]:
+        assert absb.absb_attend_workspace(_layer(), _batch(lens), _rows(new), None, opts) <= size
+    with pytest.raises(absb.AbsbError):
+        absb.absb_attend_workspace(_layer(), _batch(lens), _rows(new), None, absb.ScoreOpts(window=-1))
