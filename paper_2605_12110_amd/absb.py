@@ -558,22 +558,22 @@ def absb_rope_frequencies(rope: Rope) -> np.ndarray:
     return out[:int(rope.rot_dim) // 2].copy()
 
 
-def _rows_of_heads(t, heads: int, where: str) -> int:
-    """Row stride of a [rows][heads][d] tensor whose heads and channels are dense (None: 0)."""
-    if t is None:
-        return 0
-    if t.dim() != 3 or t.shape[1] != heads or t.stride(2) != 1 or t.stride(1) != t.shape[2]:
+def _row_stride(t, rows: int, heads: int, where: str) -> int:
+    """Of a [rows][heads][128] tensor whose heads and channels are dense."""
+    shape, stride = t.shape, t.stride()
+    if tuple(shape) != (rows, heads, 128) or stride[1] != 128 or stride[2] != 1:
         raise AbsbError(ERR_BAD_SHAPE, where)
-    return t.stride(0) if t.shape[0] > 1 else heads * t.shape[2]
+    return stride[0] if rows > 1 else heads * 128
 
 
 def absb_rotate_store(layer: Layer, rope: Rope, row_pos, row_slot, freq, q=None, q_out=None, k=None, v=None, k_cache=None,
                       v_cache=None, stream=None) -> None:
     """q, k, v: [rows][heads][128], rows any multiple of 8 elements apart (views of one projection's output, say)."""
-    cl, where = layer.c(), "absb_rotate_store"
-    qs, ks, vs = (_rows_of_heads(t, h, where) for t, h in ((q, cl.num_q_heads), (k, cl.num_kv_heads), (v, cl.num_kv_heads)))
-    n = row_pos.numel()
-    if any(t is not None and t.shape[0] != n for t in (q, q_out, k, v)) or (q_out is not None and not q_out.is_contiguous()):
+    cl, where, n = layer.c(), "absb_rotate_store", row_pos.numel()
+    qs = 0 if q is None else _row_stride(q, n, cl.num_q_heads, where)
+    ks = 0 if k is None else _row_stride(k, n, cl.num_kv_heads, where)
+    vs = 0 if v is None else _row_stride(v, n, cl.num_kv_heads, where)
+    if q_out is not None and (not q_out.is_contiguous() or q_out.numel() != n * cl.num_q_heads * 128):
         raise AbsbError(ERR_BAD_SHAPE, where)
     _check(load().absb_rotate_store(C.byref(cl), _rec(rope), n, _ptr(row_pos), _ptr(row_slot), _ptr(freq), _ptr(q), qs, _ptr(q_out),
                                     _ptr(k), ks, _ptr(v), vs, _ptr(k_cache), _ptr(v_cache), _stream(stream)), where)

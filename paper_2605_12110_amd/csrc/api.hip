@@ -916,9 +916,8 @@ static int attend(const absb_layer* layer, const absb_batch* batch, const absb_r
   if (cap > 0.0f) {
     p.cap_log2 = cap * 1.4426950408889634f;
     p.cap_in = scale / cap * 2.8853900817779268f;
-    p.cap_wide = cap > 256.0f;
   }
-  return launch_attend(p, plan, layer->dtype, cap > 0.0f, static_cast<hipStream_t>(stream));
+  return launch_attend(p, plan, layer->dtype, cap, static_cast<hipStream_t>(stream));
 }
 
 int absb_attend_rows(const absb_layer* layer, const absb_batch* batch, const absb_rows* rows, const void* q,

@@ -39,11 +39,10 @@ struct AttendParams {
   int32_t window, parts;
   float scale_log2;               // sm_scale * log2(e)
   float cap_log2, cap_in;         // cap * log2(e), 2 log2(e) sm_scale / cap (capped only)
-  int32_t cap_wide;               // 1: the cap is so far above ordinary scores that small ones need the series
   uint32_t shared_units;          // work-groups of the first phase, ahead of the second's
   AttendPhase shared, own;
 };
 
-ABSB_HIDDEN int launch_attend(const AttendParams& p, const AttendPlan& plan, int dtype, bool capped, hipStream_t stream);
+ABSB_HIDDEN int launch_attend(const AttendParams& p, const AttendPlan& plan, int dtype, float softcap, hipStream_t stream);
 
 }  // namespace absb

@@ -109,16 +109,24 @@ struct State {
   f32x16 o[4];
 };
 
-// cap tanh(y), in log2 units: cap - 2 cap / (e^2y + 1) is off by 2^-23 cap at most.
-__device__ __forceinline__ float capped(const AttendParams& p, float s) {
-  const float t = exp2_fast(s * p.cap_in);
-  return __builtin_fmaf(-2.0f * p.cap_log2, __builtin_amdgcn_rcpf(t + 1.0f), p.cap_log2);
-}
-// ... where that is too much (large caps), small y by the series.
-__device__ __forceinline__ float capped_wide(const AttendParams& p, float s) {
-  const float y = s * p.cap_in * (0.5f * LN2), z = y * y;
-  const float series = y * (1.0f + z * (-1.0f / 3 + z * (2.0f / 15 + z * (-17.0f / 315 + z * (62.0f / 2835)))));
-  return __builtin_fabsf(y) < 0.25f ? series * p.cap_log2 : capped(p, s);
+// Scores q.k in log2 units: the cap, then the distance bias (`away`: from the row to the key).  CAP_WIDE: a cap so far above
+// ordinary scores that small ones need another form.
+enum : int { CAP_NONE = 0, CAP_PLAIN = 1, CAP_WIDE = 2 };
+template <int CAP, bool BIAS>
+__device__ __forceinline__ float score_of(const AttendParams& p, float s, float slope_log2, float away) {
+  float x = s;
+  if (CAP) {
+    // cap tanh(y) = cap - 2 cap / (e^2y + 1), off by 2^-23 cap at most ...
+    const float u = s * p.cap_in;  // 2 y log2(e)
+    x = __builtin_fmaf(-2.0f * p.cap_log2, __builtin_amdgcn_rcpf(exp2_fast(u) + 1.0f), p.cap_log2);
+    if (CAP == CAP_WIDE) {  // ... or, for small y, the series
+      const float y = u * (0.5f * LN2), z = y * y;
+      const float series = y * (1.0f + z * (-1.0f / 3 + z * (2.0f / 15 + z * (-17.0f / 315 + z * (62.0f / 2835)))));
+      x = __builtin_fabsf(y) < 0.25f ? series * p.cap_log2 : x;
+    }
+  }
+  if (BIAS) x = __builtin_fmaf(-slope_log2, __builtin_fabsf(away), CAP ? x : x * p.scale_log2);
+  return x;
 }
 // Keeps the compiler from making a branch that hardly any block takes into selects that every block pays for.
 __device__ __forceinline__ void rarely() { asm volatile(""); }
@@ -138,34 +146,30 @@ __device__ __forceinline__ f32x16 scores_of(const char* kl, const u32x4 (&q)[8])
   return s;
 }
 
-// Scores of 32 KT keys from `k0` on, as products, made into what the softmax takes: in log2 units with a cap or a bias (else times
-// scale_log2, which the weights do), and -inf where a row does not see a key.  `mask`: some row of the wave does not.
-template <bool CAP, bool BIAS, int KT>
-__device__ __forceinline__ void adjust(const AttendParams& p, f32x16 (&s)[KT], int k0, bool mask, const RowOf& row, float slope_log2) {
-  const int first_key = k0 + 4 * ((threadIdx.x & 63) >> 5);
-  auto each = [&](auto f) __attribute__((always_inline)) {
+// How far a row is from key 0 of a lane's scores of the 32 keys from k0 on.  (Exact below 2^24 tokens; beyond, off by a part in 2^24.)
+__device__ __forceinline__ float away_from(const RowOf& row, int k0) {
+  return (float)(row.pos - (k0 + 4 * (int)((threadIdx.x & 63) >> 5)));
+}
+constexpr int key_of(int i) { return 8 * (i >> 2) + (i & 3); }  // score i of a lane's 16: which key behind the lane's first
+// -inf where a row does not see a key of the 32 KT from k0 on.
+template <int KT>
+__device__ __forceinline__ void hide(f32x16 (&s)[KT], int k0, const RowOf& row) {
+  const int first_key = k0 + 4 * (int)((threadIdx.x & 63) >> 5), lo = row.lo - first_key, hi = row.hi - first_key;
 #pragma unroll
-    for (int t = 0; t < KT; ++t)
+  for (int t = 0; t < KT; ++t)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[t][i] = f(s[t][i], 32 * t + 8 * (i >> 2) + (i & 3));
-  };
-  if (CAP) {
-    if (p.cap_wide) {
-      rarely();
-      each([&](float x, int) { return capped_wide(p, x); });
-    } else {
-      each([&](float x, int) { return capped(p, x); });
+    for (int i = 0; i < 16; ++i) {
+      const int at = 32 * t + key_of(i);
+      s[t][i] = at >= lo && at <= hi ? s[t][i] : -__builtin_inff();
     }
-  }
-  if (BIAS) {
-    const float d = (float)(row.pos - first_key);  // (exact below 2^24 tokens; beyond, distances are off by a part in 2^24)
-    each([&](float x, int at) { return __builtin_fmaf(-slope_log2, __builtin_fabsf(d - (float)at), CAP ? x : x * p.scale_log2); });
-  }
-  if (mask) {
-    rarely();
-    const int lo = row.lo - first_key, hi = row.hi - first_key;
-    each([&](float x, int at) { return at >= lo && at <= hi ? x : -__builtin_inff(); });
-  }
+}
+template <int CAP, bool BIAS, int KT>
+__device__ __forceinline__ void adjust(const AttendParams& p, f32x16 (&s)[KT], int k0, const RowOf& row, float slope_log2) {
+  const float away = BIAS ? away_from(row, k0) : 0.0f;
+#pragma unroll
+  for (int t = 0; t < KT; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[t][i] = score_of<CAP, BIAS>(p, s[t][i], slope_log2, away - (float)(32 * t + key_of(i)));
 }
 
 // The maximum that the rows' weights are taken against.  It follows the scores' own only when they exceed it by 2^RISE:
@@ -239,10 +243,12 @@ __device__ __forceinline__ void add_values(const char* vl, const u32x4 (&w)[2 * 
 // The main part of a step of a wide tile, in an order of its own (the compiler's would wait for every read of LDS right before its
 // product): 16 products of the next block's scores, then 16 of this block's weights with its values; beside each, the vector work
 // of one score or two, and the read that the fourth product after it needs.  A product takes the matrix unit 32 cycles, an
-// exponential the vector unit 16, its other work 12.  `mx`: the largest of a lane's next scores.
-template <int DT, bool SCALED>
+// exponential the vector unit 16, its other work 12.  `mx`: the largest of a lane's next scores; `away`: of the row from their
+// first key.
+template <int DT, int CAP, bool BIAS>
 __device__ __forceinline__ void wide_step(const AttendParams& p, const char* kl, const char* vl, const u32x4 (&q)[8], const f32x16 (&s)[2],
-                                          float base, f32x16 (&s_next)[2], float& mx, State& st) {
+                                          float base, f32x16 (&s_next)[2], float& mx, State& st, float slope_log2, float away) {
+  constexpr bool SCALED = CAP || BIAS;  // (else the scores are still q.k)
   constexpr int AHEAD = 4, SLOTS = 32;
   const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5, i16 = lane & 15, grp = (lane >> 4) & 1;
   u32x4 f[AHEAD], w[4];
@@ -286,9 +292,15 @@ __device__ __forceinline__ void wide_step(const AttendParams& p, const char* kl,
         x = y;
       }
     }
-    if (!SCALED && j >= 20 && j < 28) {
+    // the next scores, which the sixteenth product has completed: what the softmax takes, and their maximum
+    if (j >= 18) {
 #pragma unroll
-      for (int e = (j - 20) * 4; e < (j - 19) * 4; ++e) mx = fmaxf(mx, s_next[e >> 4][e & 15]);
+      for (int e = (j - 18) * 16 / 7; e < (j - 17) * 16 / 7; ++e) {
+        float y = s_next[e >> 4][e & 15];
+        if (SCALED) y = score_of<CAP, BIAS>(p, y, slope_log2, away - (float)(32 * (e >> 4) + key_of(e & 15)));
+        s_next[e >> 4][e & 15] = y;
+        mx = fmaxf(mx, y);
+      }
     }
     asm volatile("" : "+v"(sum0), "+v"(sum1));  // (the sums are made here, not out of 32 kept values at the end)
     __builtin_amdgcn_sched_barrier(0);
@@ -418,7 +430,7 @@ __device__ __forceinline__ RowOf row_of(const AttendParams& p, const Tile& t, bo
 
 constexpr int ATT_LDS = 65536;  // wide: a block of 64 keys, twice; narrow: 32 keys a wave, and later the waves' outputs
 
-template <int DT, bool CAP, bool BIAS>
+template <int DT, int CAP, bool BIAS>
 __global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) {
   __shared__ __align__(16) char s_kv[ATT_LDS];
   __shared__ float s_ml[ATT_WAVES][2][32];
@@ -532,6 +544,7 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) 
         s0[0] = scores_of<DT>(mine, q);
         s0[1] = scores_of<DT>(mine + 32 * ROW_BYTES, q);
       }
+      if (SCALED) adjust<CAP, BIAS, 2>(p, s0, begin, row, slope_log2);
       float mx = live ? largest<2>(s0) : 0.0f;
       auto step = [&](int i, f32x16 (&s)[2], f32x16 (&s_next)[2]) __attribute__((always_inline)) {
         const char *kl = mine + ((i + 1) & 1) * STAGE, *vl = mine + 2 * STAGE + (i & 1) * STAGE;
@@ -548,14 +561,13 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) 
         }
         if (!live) return;
         const int k0 = begin + i * STEP;
-        const bool mask = k0 < all_lo || k0 + 63 > all_hi;
-        if (SCALED || mask) {
+        if (k0 < all_lo || k0 + 63 > all_hi) {
           rarely();
-          adjust<CAP, BIAS, 2>(p, s, k0, mask, row, slope_log2);
+          hide<2>(s, k0, row);
           mx = largest<2>(s);
         }
         const float base = new_maximum<SCALED>(p, mx, st);
-        wide_step<DT, SCALED>(p, kl, vl, q, s, base, s_next, mx, st);
+        wide_step<DT, CAP, BIAS>(p, kl, vl, q, s, base, s_next, mx, st, slope_log2, BIAS ? away_from(row, k0 + STEP) : 0.0f);
       };
       for (int i = 0; i < steps; i += 2) {
         step(i, s0, s1);
@@ -590,7 +602,11 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) 
         u32x4 w[2];
         if (live) {
           // (a split ends on a block or with the tile's last key, so what a row sees of a block is in its interval)
-          adjust<CAP, BIAS, 1>(p, s, k0, k0 < all_lo || k1 > all_hi, row, slope_log2);
+          if (SCALED) adjust<CAP, BIAS, 1>(p, s, k0, row, slope_log2);
+          if (k0 < all_lo || k1 > all_hi) {
+            rarely();
+            hide<1>(s, k0, row);
+          }
           const float base = new_maximum<SCALED>(p, largest<1>(s), st);
           weigh<DT, SCALED, 1>(p, s, base, w, st);
         }
@@ -717,7 +733,7 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(AttendParams p, int64
   if (p.lse && lane == 0) p.lse[at] = L > 0.0f ? (M + __builtin_log2f(L)) * LN2 : -__builtin_inff();
 }
 
-template <int DT, bool CAP, bool BIAS>
+template <int DT, int CAP, bool BIAS>
 static void launch_parts(const AttendParams& p, int64_t rows, hipStream_t stream) {
   const int64_t own_units = p.own.slots * p.Hkv * p.own.splits;
   hipLaunchKernelGGL((attend_kernel<DT, CAP, BIAS>), dim3((unsigned)(p.shared_units + own_units)), dim3(ATT_THREADS), 0, stream, p);
@@ -726,23 +742,28 @@ static void launch_parts(const AttendParams& p, int64_t rows, hipStream_t stream
     hipLaunchKernelGGL((attend_merge_kernel<DT>), dim3((unsigned)((pairs + 3) / 4)), dim3(256), 0, stream, p, pairs);
   }
 }
-template <int DT>
-static void launch_typed(const AttendParams& p, const AttendPlan& plan, bool capped, hipStream_t stream) {
-  if (capped && p.slopes)
-    launch_parts<DT, true, true>(p, plan.rows, stream);
-  else if (capped)
-    launch_parts<DT, true, false>(p, plan.rows, stream);
-  else if (p.slopes)
-    launch_parts<DT, false, true>(p, plan.rows, stream);
+template <int DT, int CAP>
+static void launch_capped(const AttendParams& p, int64_t rows, hipStream_t stream) {
+  if (p.slopes)
+    launch_parts<DT, CAP, true>(p, rows, stream);
   else
-    launch_parts<DT, false, false>(p, plan.rows, stream);
+    launch_parts<DT, CAP, false>(p, rows, stream);
+}
+template <int DT>
+static void launch_typed(const AttendParams& p, const AttendPlan& plan, float softcap, hipStream_t stream) {
+  if (softcap == 0.0f)
+    launch_capped<DT, CAP_NONE>(p, plan.rows, stream);
+  else if (softcap <= 256.0f)  // (its rounding error, in units of a score: 256 / 2^23)
+    launch_capped<DT, CAP_PLAIN>(p, plan.rows, stream);
+  else
+    launch_capped<DT, CAP_WIDE>(p, plan.rows, stream);
 }
 
-int launch_attend(const AttendParams& p, const AttendPlan& plan, int dtype, bool capped, hipStream_t stream) {
+int launch_attend(const AttendParams& p, const AttendPlan& plan, int dtype, float softcap, hipStream_t stream) {
   if (dtype == ABSB_F16)
-    launch_typed<ABSB_F16>(p, plan, capped, stream);
+    launch_typed<ABSB_F16>(p, plan, softcap, stream);
   else
-    launch_typed<ABSB_BF16>(p, plan, capped, stream);
+    launch_typed<ABSB_BF16>(p, plan, softcap, stream);
   return check_launch();
 }
 

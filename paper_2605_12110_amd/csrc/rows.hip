@@ -15,34 +15,41 @@ namespace absb {
 // rows, of the fresh pages and of the pages given back, so that none waits for another.  Nothing written here is
 // read here: a row in a fresh page takes it from the ring, not from the table.  The cursors change at the end of the call only,
 // written by the work-group that finishes last, since until then others may be reading them.
-constexpr int MAP_THREADS = 1024;
-
+//
+// Bound by latency: lengths in, page table or ring in, rows out, and two barriers between.  256 threads while they cover the batch
+// (64 requests: 5.6 us with 1024, 16 waves at every barrier), else 1024.
 struct MapSums {
   int32_t rows, take, give;  // of the requests before a point
 };
 
-__global__ __launch_bounds__(MAP_THREADS) void map_rows_kernel(MapParams p) {
-  __shared__ int32_t s_rows[MAP_THREADS + 1], s_take[MAP_THREADS + 1], s_give[MAP_THREADS + 1];
-  __shared__ int32_t s_before[MAP_THREADS], s_had[MAP_THREADS], s_need[MAP_THREADS];
-  __shared__ int32_t s_wave[3][MAP_THREADS / 64], s_short;
+template <int T>
+__global__ __launch_bounds__(T) void map_rows_kernel(MapParams p) {
+  constexpr int WAVES = T / 64;
+  __shared__ int32_t s_rows[T + 1], s_take[T + 1], s_give[T + 1];
+  __shared__ int32_t s_before[T], s_had[T], s_need[T];
+  __shared__ int32_t s_wave[4][WAVES];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int lP = p.log2_page, P = 1 << lP;
+  const bool ring = p.ring != nullptr;
+  const uint32_t cap = (uint32_t)p.capacity;
+  int64_t head = 0, tail = 0;
+  if (ring) {
+    head = p.cursors[0];
+    tail = p.cursors[1];
+  }
 
-  int before = 0, after = 0;
-  auto read = [&](int b) {
-    before = b < p.batch ? max(p.before[b], 0) : 0;
-    after = b < p.batch ? max(p.after[b], 0) : 0;
-  };
-  auto pages_of = [&](int len) { return (int)(((int64_t)len + P - 1) >> lP); };
-  // Prefix sums over the MAP_THREADS requests from b0 on, into s_*[0 .. MAP_THREADS]; the requests' own values beside them.
-  auto scan = [&](int b0) {
-    read(b0 + tid);
-    const int had = pages_of(before), need = pages_of(after);
-    const uint32_t v[3] = {(uint32_t)max(after - before, 0), (uint32_t)max(need - had, 0), (uint32_t)max(had - need, 0)};
-    uint32_t in[3];
-    __syncthreads();  // what the last chunk left has been read
+  // Prefix sums over the T requests from b0 on, into s_*[0 .. T]; the requests' own values beside them.  Returns how many pages
+  // the tables have no place for.
+  auto scan = [&](int b0, bool first) __attribute__((always_inline)) {
+    const int b = b0 + tid;
+    const int before = b < p.batch ? max(p.before[b], 0) : 0, after = b < p.batch ? max(p.after[b], 0) : 0;
+    const int had = (int)(((int64_t)before + P - 1) >> lP), need = (int)(((int64_t)after + P - 1) >> lP);
+    const uint32_t v[4] = {(uint32_t)max(after - before, 0), (uint32_t)max(need - had, 0), (uint32_t)max(had - need, 0),
+                           ring ? (uint32_t)max(0, need - max(p.pt_stride, had)) : 0u};
+    uint32_t in[4];
+    if (!first) __syncthreads();  // what the last chunk left has been read
 #pragma unroll
-    for (int k = 0; k < 3; ++k) {
+    for (int k = 0; k < 4; ++k) {
       uint32_t total;
       in[k] = wave_incl_scan_u32(v[k], &total);
       if (lane == 0) s_wave[k][wave] = (int32_t)total;
@@ -51,100 +58,100 @@ __global__ __launch_bounds__(MAP_THREADS) void map_rows_kernel(MapParams p) {
     s_had[tid] = had;
     s_need[tid] = need;
     __syncthreads();
+    int short_of = 0;
 #pragma unroll
-    for (int k = 0; k < 3; ++k)
-      for (int w = 0; w < wave; ++w) in[k] += (uint32_t)s_wave[k][w];
+    for (int w = 0; w < WAVES; ++w) {
+#pragma unroll
+      for (int k = 0; k < 3; ++k) in[k] += w < wave ? (uint32_t)s_wave[k][w] : 0u;
+      short_of += s_wave[3][w];
+    }
     s_rows[tid + 1] = (int32_t)in[0];
     s_take[tid + 1] = (int32_t)in[1];
     s_give[tid + 1] = (int32_t)in[2];
     if (tid == 0) s_rows[0] = s_take[0] = s_give[0] = 0;
     __syncthreads();
+    return short_of;
   };
-  // Largest i in [0, MAP_THREADS) with s[i] <= x (s[0] = 0 <= x < s[MAP_THREADS]): the request that x falls to.
-  auto owner = [&](const int32_t* s, int x) {
+  // Largest i in [0, T) with s[i] <= x (s[0] = 0 <= x < s[T]): the request that x falls to.
+  auto owner = [&](const int32_t* s, int x) __attribute__((always_inline)) {
     int lo = 0;
 #pragma unroll
-    for (int step = MAP_THREADS / 2; step > 0; step >>= 1)
+    for (int step = T / 2; step > 0; step >>= 1)
       if (s[lo + step] <= x) lo += step;
     return lo;
   };
 
   // ---- the sums of the whole batch, and whether every page can be had
-  const bool one_chunk = p.batch <= MAP_THREADS;
+  const bool one_chunk = p.batch <= T;
   MapSums all = {0, 0, 0};
-  int too_long = 0;
-  for (int b0 = 0; b0 < p.batch; b0 += MAP_THREADS) {
-    scan(b0);
-    if (p.ring) too_long += max(0, s_need[tid] - max(p.pt_stride, s_had[tid]));  // pages that its table row has no place for
-    all.rows += s_rows[MAP_THREADS];
-    all.take += s_take[MAP_THREADS];
-    all.give += s_give[MAP_THREADS];
+  int64_t missing = 0;
+  for (int b0 = 0; b0 < p.batch; b0 += T) {
+    missing += scan(b0, b0 == 0);
+    all.rows += s_rows[T];
+    all.take += s_take[T];
+    all.give += s_give[T];
   }
-  int64_t head = 0, tail = 0, missing = 0;
-  if (p.ring) {
-    head = p.cursors[0];
-    tail = p.cursors[1];
-    if (tid == 0) s_short = 0;
-    __syncthreads();
-    if (too_long) atomicAdd(&s_short, too_long);
-    __syncthreads();
-    missing = max((int64_t)0, (int64_t)all.take - (tail - head)) + s_short;
-  }
+  if (ring) missing += max((int64_t)0, (int64_t)all.take - (tail - head));
   const bool fine = missing == 0;
+  // entry `from` + i of the ring: no division but this one
+  auto first_place = [&](int64_t from) { return (uint64_t)from >> 32 ? (uint32_t)((uint64_t)from % cap) : (uint32_t)from % cap; };
+  const uint32_t head0 = ring ? first_place(head) : 0, tail0 = ring ? first_place(tail) : 0;
+  auto place = [&](uint32_t first, int i) __attribute__((always_inline)) {
+    const uint64_t at = (uint64_t)first + (uint32_t)i;
+    return at < cap ? (uint32_t)at : at - cap < cap ? (uint32_t)(at - cap) : (uint32_t)(at % cap);
+  };
 
   // ---- this work-group's share of the rows, the fresh pages and the pages given back
   const int nwg = gridDim.x, wg = blockIdx.x;
-  auto share = [&](int64_t n, int* from, int* to) {
-    const int64_t each = (n + nwg - 1) / nwg;
-    *from = (int)min(n, wg * each);
-    *to = (int)min(n, (wg + 1) * each);
+  struct Share {
+    int from, to;
   };
-  int r_from, r_to, t_from, t_to, g_from, g_to;
-  share(min(all.rows, p.max_rows), &r_from, &r_to);
-  share(p.ring && fine ? all.take : 0, &t_from, &t_to);
-  share(p.ring && fine ? all.give : 0, &g_from, &g_to);
+  auto share = [&](int n) __attribute__((always_inline)) {
+    if (nwg == 1) return Share{0, n};
+    const uint32_t each = ((uint32_t)n + nwg - 1) / (uint32_t)nwg;
+    return Share{(int)min((uint64_t)n, (uint64_t)wg * each), (int)min((uint64_t)n, (uint64_t)(wg + 1) * each)};
+  };
+  const Share r = share(min(all.rows, p.max_rows)), take = share(ring && fine ? all.take : 0), give = share(ring && fine ? all.give : 0);
   MapSums base = {0, 0, 0};
-  for (int b0 = 0; b0 < p.batch; b0 += MAP_THREADS) {
-    if (!one_chunk) scan(b0);  // (else it is still there)
-    const int nb = min(MAP_THREADS, p.batch - b0);
-    if (wg == 0 && tid < nb) p.row_off[b0 + tid] = base.rows + s_rows[tid];
-    const int r_end = min(r_to, base.rows + s_rows[MAP_THREADS]);
-    for (int r = max(r_from, base.rows) + tid; r < r_end; r += MAP_THREADS) {
-      const int i = owner(s_rows, r - base.rows), pos = s_before[i] + (r - base.rows - s_rows[i]), page = pos >> lP;
+  for (int b0 = 0; b0 < p.batch; b0 += T) {
+    if (!one_chunk) scan(b0, false);  // (else it is still there)
+    if (wg == 0 && tid < p.batch - b0) p.row_off[b0 + tid] = base.rows + s_rows[tid];
+    const int r_end = min(r.to, base.rows + s_rows[T]);
+    for (int x = max(r.from, base.rows) + tid; x < r_end; x += T) {
+      const int i = owner(s_rows, x - base.rows), pos = s_before[i] + (x - base.rows - s_rows[i]), page = pos >> lP;
+      const bool fresh = ring && page >= s_had[i];
       int64_t slot = -1;
-      const bool fresh = p.ring && page >= s_had[i];
       if (fine && (fresh || page < p.pt_stride)) {
-        const int32_t phys = fresh
-                                 ? p.ring[(head + base.take + s_take[i] + page - s_had[i]) % p.capacity]
-                                 : p.page_table[(int64_t)(b0 + i) * p.pt_stride + page];
-        slot = ((int64_t)phys << lP) + (pos & (P - 1));
+        const int32_t* at = fresh ? p.ring + place(head0, base.take + s_take[i] + page - s_had[i])
+                                  : p.page_table + ((int64_t)(b0 + i) * p.pt_stride + page);
+        slot = ((int64_t)*at << lP) + (pos & (P - 1));
       }
-      p.row_pos[r] = pos;
-      p.row_slot[r] = slot;
+      p.row_pos[x] = pos;
+      p.row_slot[x] = slot;
     }
-    const int t_end = min(t_to, base.take + s_take[MAP_THREADS]);
-    for (int t = max(t_from, base.take) + tid; t < t_end; t += MAP_THREADS) {
-      const int i = owner(s_take, t - base.take), page = s_had[i] + (t - base.take - s_take[i]);
-      p.page_table[(int64_t)(b0 + i) * p.pt_stride + page] = p.ring[(head + t) % p.capacity];
+    const int t_end = min(take.to, base.take + s_take[T]);
+    for (int x = max(take.from, base.take) + tid; x < t_end; x += T) {
+      const int i = owner(s_take, x - base.take), page = s_had[i] + (x - base.take - s_take[i]);
+      p.page_table[(int64_t)(b0 + i) * p.pt_stride + page] = p.ring[place(head0, x)];
     }
-    const int g_end = min(g_to, base.give + s_give[MAP_THREADS]);
-    for (int t = max(g_from, base.give) + tid; t < g_end; t += MAP_THREADS) {
-      const int i = owner(s_give, t - base.give), page = s_need[i] + (t - base.give - s_give[i]);
-      if (page < p.pt_stride) p.ring[(tail + t) % p.capacity] = p.page_table[(int64_t)(b0 + i) * p.pt_stride + page];
+    const int g_end = min(give.to, base.give + s_give[T]);
+    for (int x = max(give.from, base.give) + tid; x < g_end; x += T) {
+      const int i = owner(s_give, x - base.give), page = s_need[i] + (x - base.give - s_give[i]);
+      if (page < p.pt_stride) p.ring[place(tail0, x)] = p.page_table[(int64_t)(b0 + i) * p.pt_stride + page];
     }
-    base.rows += s_rows[MAP_THREADS];
-    base.take += s_take[MAP_THREADS];
-    base.give += s_give[MAP_THREADS];
+    base.rows += s_rows[T];
+    base.take += s_take[T];
+    base.give += s_give[T];
   }
   if (wg == 0 && tid == 0) p.row_off[p.batch] = all.rows;
-  int f_from, f_to;  // rows behind the last one
-  share(max(0, p.max_rows - all.rows), &f_from, &f_to);
-  for (int r = all.rows + f_from + tid; r < all.rows + f_to; r += MAP_THREADS) {
-    p.row_pos[r] = 0;
-    p.row_slot[r] = -1;
+  const Share fill = share(max(0, p.max_rows - all.rows));  // rows behind the last one
+  for (int x = fill.from + tid; x < fill.to; x += T) {
+    p.row_pos[all.rows + x] = 0;
+    p.row_slot[all.rows + x] = -1;
   }
-  if (!p.ring) return;
-  __syncthreads();  // (the cursors have been read by all of the work-group long since)
+  if (!ring) return;
+  // The cursors: by the work-group that comes last, since all the others have read them by then.
+  if (nwg > 1) __syncthreads();
   if (tid == 0) {
     unsigned long long* done = reinterpret_cast<unsigned long long*>(p.cursors_out + 3);
     if (nwg == 1 || __hip_atomic_fetch_add(done, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned long long)nwg - 1) {
@@ -157,10 +164,16 @@ __global__ __launch_bounds__(MAP_THREADS) void map_rows_kernel(MapParams p) {
 }
 
 int launch_map_rows(const MapParams& p, hipStream_t stream) {
-  const int64_t items = (int64_t)p.max_rows + p.batch;
-  const int64_t wgs = items <= 2 * MAP_THREADS ? 1 : items / MAP_THREADS;
-  const int grid = (int)(wgs < 256 ? wgs : 256);
-  hipLaunchKernelGGL(map_rows_kernel, dim3(grid), dim3(MAP_THREADS), 0, stream, p);
+  // a row or two a thread, at most a work-group a compute unit
+  const int threads = p.batch <= 256 ? 256 : p.batch <= 512 ? 512 : 1024;
+  const int wgs = p.max_rows <= 2 * threads ? 1 : p.max_rows / threads;
+  const int grid = wgs < 256 ? wgs : 256;
+  if (threads == 256)
+    hipLaunchKernelGGL((map_rows_kernel<256>), dim3(grid), dim3(256), 0, stream, p);
+  else if (threads == 512)
+    hipLaunchKernelGGL((map_rows_kernel<512>), dim3(grid), dim3(512), 0, stream, p);
+  else
+    hipLaunchKernelGGL((map_rows_kernel<1024>), dim3(grid), dim3(1024), 0, stream, p);
   return check_launch();
 }
 
@@ -190,29 +203,25 @@ __device__ __forceinline__ void sin_cos(uint64_t F, int32_t pos, float amplitude
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-// Where head h of a row is read from and written to (queries, then keys, then values).
-struct HeadIo {
-  const uint16_t* src;
-  uint16_t* dst;  // null: nowhere
-  bool turn;
-};
-__device__ __forceinline__ HeadIo head_io(const RotateParams& p, int row, int h, int64_t slot) {
-  HeadIo io;
-  if (h < p.nq) {
-    io.src = p.q + row * p.q_stride + h * ABSB_HEAD_DIM;
-    io.dst = p.q_out + ((int64_t)row * p.nq + h) * ABSB_HEAD_DIM;
-    io.turn = true;
-    return io;
-  }
+// Where head h of a row is read from and written to (queries, then keys, then values; null: nowhere).
+__device__ __forceinline__ const uint16_t* head_src(const RotateParams& p, int row, int h) {
+  if (h < p.nq) return p.q + row * p.q_stride + h * ABSB_HEAD_DIM;
+  h -= p.nq;
+  return h < p.nkv ? p.k + row * p.k_stride + h * ABSB_HEAD_DIM : p.v + row * p.v_stride + (h - p.nkv) * ABSB_HEAD_DIM;
+}
+__device__ __forceinline__ uint16_t* head_dst(const RotateParams& p, int row, int h, int64_t slot) {
+  if (h < p.nq) return p.q_out + ((int64_t)row * p.nq + h) * ABSB_HEAD_DIM;
+  if (slot < 0) return nullptr;
   h -= p.nq;
   const bool key = h < p.nkv;
-  if (!key) h -= p.nkv;
-  io.src = (key ? p.k + row * p.k_stride : p.v + row * p.v_stride) + h * ABSB_HEAD_DIM;
-  uint16_t* cache = key ? p.k_cache : p.v_cache;
-  io.dst = slot < 0 ? nullptr
-                    : cache + (slot >> p.log2_page) * p.s_page + (int64_t)h * p.s_head + (slot & ((1 << p.log2_page) - 1)) * p.s_tok;
-  io.turn = key;
-  return io;
+  return (key ? p.k_cache : p.v_cache) + (slot >> p.log2_page) * p.s_page + (int64_t)(key ? h : h - p.nkv) * p.s_head +
+         (slot & ((1 << p.log2_page) - 1)) * p.s_tok;
+}
+// Two values rounded to the K/V type, side by side.
+template <int DT>
+__device__ __forceinline__ uint32_t pair_of(float a, float b) {
+  if (DT == ABSB_F16) return bitcast<uint32_t>(half2_t{(_Float16)a, (_Float16)b});
+  return bitcast<uint32_t>(bf16x2_t{(__bf16)a, (__bf16)b});
 }
 
 // Halves of whole pieces (rot_dim a multiple of 16), or neighbours (of 8): LANES lanes a head.
@@ -229,6 +238,16 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateParams p) {
   const bool turns = piece < turned;
   const int ca = (PAIRS || turns ? piece : piece + turned) * 8, cb = (piece + turned) * 8;
   const bool used = ca < ABSB_HEAD_DIM;
+  // A head's pieces are asked for ahead of what is done with them: the first ahead of the sines, the next ahead of the one before.
+  u32x4 a = {0u, 0u, 0u, 0u}, b = a;
+  const bool two = !PAIRS && turns;
+  auto fetch = [&](int h) __attribute__((always_inline)) {
+    if (h >= h_end || !used) return;
+    const uint16_t* src = head_src(p, row, h);
+    a = *reinterpret_cast<const u32x4*>(src + ca);
+    if (two) b = *reinterpret_cast<const u32x4*>(src + cb);
+  };
+  fetch(h0);
   const int pos = p.pos[row];
   const int64_t slot = p.slot ? p.slot[row] : -1;
   constexpr int N = PAIRS ? 4 : 8;  // pairs of a lane
@@ -240,28 +259,26 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateParams p) {
     if (turns) sin_cos(turns_of(p.freq[piece * N + i]), pos, p.amplitude, &sn[i], &cs[i]);
   }
   for (int h = h0; h < h_end; h += HEADS) {
-    const HeadIo io = head_io(p, row, h, slot);
-    if (!io.dst || !used) continue;
-    u32x4 a = *reinterpret_cast<const u32x4*>(io.src + ca), b = {0u, 0u, 0u, 0u};
-    const bool two = !PAIRS && turns;
-    if (two) b = *reinterpret_cast<const u32x4*>(io.src + cb);
-    if (io.turn && turns) {
+    u32x4 x = a, y = b;
+    fetch(h + HEADS);
+    uint16_t* dst = head_dst(p, row, h, slot);
+    if (!dst || !used) continue;
+    if (turns && h < p.nq + p.nkv) {
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
         if (PAIRS) {
-          const float x = Elem<DT>::lo(a[w]), y = Elem<DT>::hi(a[w]);
-          const float u = x * cs[w % N] - y * sn[w % N], v = x * sn[w % N] + y * cs[w % N];
-          a[w] = (uint32_t)Elem<DT>::narrow(u) | ((uint32_t)Elem<DT>::narrow(v) << 16);
+          const float u = Elem<DT>::lo(x[w]), v = Elem<DT>::hi(x[w]);
+          x[w] = pair_of<DT>(u * cs[w % N] - v * sn[w % N], u * sn[w % N] + v * cs[w % N]);
         } else {
-          const float x0 = Elem<DT>::lo(a[w]), y0 = Elem<DT>::lo(b[w]), x1 = Elem<DT>::hi(a[w]), y1 = Elem<DT>::hi(b[w]);
+          const float x0 = Elem<DT>::lo(x[w]), y0 = Elem<DT>::lo(y[w]), x1 = Elem<DT>::hi(x[w]), y1 = Elem<DT>::hi(y[w]);
           const int i = 2 * w % N, j = (2 * w + 1) % N;
-          a[w] = (uint32_t)Elem<DT>::narrow(x0 * cs[i] - y0 * sn[i]) | ((uint32_t)Elem<DT>::narrow(x1 * cs[j] - y1 * sn[j]) << 16);
-          b[w] = (uint32_t)Elem<DT>::narrow(x0 * sn[i] + y0 * cs[i]) | ((uint32_t)Elem<DT>::narrow(x1 * sn[j] + y1 * cs[j]) << 16);
+          x[w] = pair_of<DT>(x0 * cs[i] - y0 * sn[i], x1 * cs[j] - y1 * sn[j]);
+          y[w] = pair_of<DT>(x0 * sn[i] + y0 * cs[i], x1 * sn[j] + y1 * cs[j]);
         }
       }
     }
-    *reinterpret_cast<u32x4*>(io.dst + ca) = a;
-    if (two) *reinterpret_cast<u32x4*>(io.dst + cb) = b;
+    *reinterpret_cast<u32x4*>(dst + ca) = x;
+    if (two) *reinterpret_cast<u32x4*>(dst + cb) = y;
   }
 }
 
@@ -280,16 +297,17 @@ __global__ __launch_bounds__(256) void rotate_any_kernel(RotateParams p) {
   float sn = 0.0f, cs = 1.0f;
   if (turns) sin_cos(turns_of(p.freq[lane]), p.pos[row], p.amplitude, &sn, &cs);
   for (int h = part * p.heads_per_part; h < h_end; ++h) {
-    const HeadIo io = head_io(p, row, h, slot);
-    if (!io.dst) continue;
-    uint16_t a = io.src[ca], b = io.src[cb];
-    if (io.turn && turns) {
+    uint16_t* dst = head_dst(p, row, h, slot);
+    if (!dst) continue;
+    const uint16_t* src = head_src(p, row, h);
+    uint16_t a = src[ca], b = src[cb];
+    if (turns && h < p.nq + p.nkv) {
       const float x = Elem<DT>::widen(a), y = Elem<DT>::widen(b);
       a = Elem<DT>::narrow(x * cs - y * sn);
       b = Elem<DT>::narrow(x * sn + y * cs);
     }
-    io.dst[ca] = a;
-    io.dst[cb] = b;
+    dst[ca] = a;
+    dst[cb] = b;
   }
 }
 

@@ -97,12 +97,9 @@ class _T:
     def element_size(self):
         return self._size
 
-    def dim(self):
-        return len(self.shape)
-
-    def stride(self, i):
-        dense = math.prod(self.shape[i + 1:])
-        return self._s0 if i == 0 and self._s0 is not None else dense
+    def stride(self):
+        dense = tuple(math.prod(self.shape[i + 1:]) for i in range(len(self.shape)))
+        return dense if self._s0 is None else (self._s0, *dense[1:])
 
     def is_contiguous(self):
         return self._s0 is None
