@@ -393,6 +393,7 @@ static int plan_attend(const absb_layer* layer, const absb_batch* batch, const a
     max_n = std::max<int64_t>(max_n, off[b + 1] - off[b]);
   }
   if ((int64_t)batch->pt_stride < ceil_div(max_len, P)) return ABSB_ERR_BAD_SHAPE;
+  if ((int64_t)off[Bt] * layer->num_q_heads >= int64_t(1) << 31) return ABSB_ERR_BAD_SHAPE;  // (queries of half a terabyte)
   AttendPlan p = {};
   p.rows = off[Bt];
   PhaseSums sums[2];  // shared keys, own keys
@@ -480,7 +481,6 @@ static int plan_attend(const absb_layer* layer, const absb_batch* batch, const a
   const int ws_parts = any_options ? parts_any : p.parts;
   if (p.shared.slots * Hkv * p.shared.splits + p.own.slots * Hkv * p.own.splits >= (int64_t(1) << 31)) return ABSB_ERR_BAD_SHAPE;
   const int64_t pairs = p.rows * layer->num_q_heads;
-  if (ceil_div(pairs, 4) >= (int64_t(1) << 31)) return ABSB_ERR_BAD_SHAPE;
   if (ws_parts > 1) {
     p.ws_part_ml = align256((size_t)pairs * ws_parts * ABSB_HEAD_DIM * 4);
     p.ws_bytes = p.ws_part_ml + align256((size_t)pairs * ws_parts * 2 * 4);
@@ -906,6 +906,7 @@ static int attend(const absb_layer* layer, const absb_batch* batch, const absb_r
   p.Hq = layer->num_q_heads;
   p.Hkv = layer->num_kv_heads;
   p.G = p.Hq / p.Hkv;
+  p.inv_G = (65536 + p.G - 1) / p.G;
   p.log2_page = ilog2(layer->page_size);
   p.parts = plan.parts;
   p.shared = plan.shared;

@@ -36,6 +36,7 @@ struct AttendParams {
   float* part_ml;  // [rows][Hq][parts][2]: maximum in log2 units, sum
   int64_t s_page, s_head, s_tok;  // bytes
   int32_t batch, groups, pt_stride, Hq, Hkv, G, log2_page;
+  int32_t inv_G;                  // 2^16 / G, rounded up
   int32_t window, parts;
   float scale_log2;               // sm_scale * log2(e)
   float cap_log2, cap_in;         // cap * log2(e), 2 log2(e) sm_scale / cap (capped only)

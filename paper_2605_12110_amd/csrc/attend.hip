@@ -61,10 +61,10 @@ __device__ __forceinline__ float across_halves(float x, Op op) {
 // The owner of tile slot x: the largest o in [0, n) with slot0(o) <= x, where slot0(o) = row0(o) * G / tile + o, and its rows
 // [row0(o), row0(o + 1)).  The wave looks at 64 places at a time; up to 63 owners are one look.
 struct Owner {
-  int o, r0, r1;
+  int o, r0, r1, len;  // ... and lens[o]
 };
 template <typename F>
-__device__ __forceinline__ Owner owner_of(int n, int64_t x, int G, int log2_tile, F row0) {
+__device__ __forceinline__ Owner owner_of(int n, int64_t x, int G, int log2_tile, const int32_t* lens, F row0) {
   const int lane = threadIdx.x & 63;
   int lo = 0, hi = n;  // the owner is in [lo, hi)
   while (hi - lo > 63) {
@@ -73,22 +73,27 @@ __device__ __forceinline__ Owner owner_of(int n, int64_t x, int G, int log2_tile
     lo += (__popcll(below) - 1) * step;
     hi = min(hi, lo + step);
   }
-  const int at = min(lo + lane, hi), r = row0(at);
+  const int at = min(lo + lane, hi), r = row0(at), len = lens[min(at, n - 1)];
   const uint64_t below = __ballot(lo + lane < hi && (((int64_t)r * G) >> log2_tile) + at <= x);
   const int i = __popcll(below) - 1;
-  return Owner{lo + i, __builtin_amdgcn_readlane(r, i), __builtin_amdgcn_readlane(r, i + 1)};
+  return Owner{lo + i, __builtin_amdgcn_readlane(r, i), __builtin_amdgcn_readlane(r, i + 1), __builtin_amdgcn_readlane(len, i)};
 }
-// The shared tokens of request b: those of the last group g with first[g] <= b.
-__device__ __forceinline__ int shared_tokens(const AttendParams& p, int b) {
+// The shared tokens of request b: those of the last group g with first[g] <= b.  `first`, `len`: the lane's group of the first 64,
+// asked for beforehand.
+__device__ __forceinline__ int shared_tokens(const AttendParams& p, int b, int first, int len) {
   const int lane = threadIdx.x & 63;
   int lo = 0, hi = p.groups;
   while (hi - lo > 64) {
     const int step = (hi - lo + 63) >> 6, at = lo + lane * step;
     lo += (__popcll(__ballot(at < hi && p.first[min(at, hi - 1)] <= b)) - 1) * step;
     hi = min(hi, lo + step);
+    if (hi - lo <= 64) {
+      const int mine = min(lo + lane, hi - 1);
+      first = p.first[mine];
+      len = p.len[mine];
+    }
   }
-  const int at = min(lo + lane, hi - 1), len = p.len[at];
-  return __builtin_amdgcn_readlane(len, __popcll(__ballot(lo + lane < hi && p.first[at] <= b)) - 1);
+  return __builtin_amdgcn_readlane(len, __popcll(__ballot(lo + lane < hi && first <= b)) - 1);
 }
 
 struct RowOf {
@@ -99,8 +104,9 @@ struct RowOf {
 // What a work-group's tile is about.
 struct Tile {
   int table_row, limit;     // whose page-table row; keys it holds
-  int r0, n;                // first row, rows (tokens)
-  int64_t f0;               // first (token, head) pair of the tile
+  int r0, n;                // the owner's first row, rows (tokens)
+  int tok0, g0;             // the tile's first (token, head) pair
+  int pairs;                // of the owner from there on
 };
 
 // Softmax state and output of a wave's 32 rows: lane l holds row l % 32; O[t][i] is channel 32 t + 8 (i / 4) + 4 (l / 32) + i % 4.
@@ -131,19 +137,18 @@ __device__ __forceinline__ float score_of(const AttendParams& p, float s, float 
 // Keeps the compiler from making a branch that hardly any block takes into selects that every block pays for.
 __device__ __forceinline__ void rarely() { asm volatile(""); }
 
-// S^T of the 32 keys whose K rows are at `kl`: score i of a lane is of key 8 (i / 4) + 4 half + i % 4.
+// S^T of the 32 keys whose K rows are at `kl`: score i of a lane is of key 8 (i / 4) + 4 half + i % 4.  (Two chains of products: a
+// lone wave waits for each of a chain.)
 template <int DT>
 __device__ __forceinline__ f32x16 scores_of(const char* kl, const u32x4 (&q)[8]) {
   const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
-  f32x16 s;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+  f32x16 s[2] = {};
 #pragma unroll
   for (int c = 0; c < 8; ++c) {
     const u32x4 a = *reinterpret_cast<const u32x4*>(kl + col * ROW_BYTES + (((2 * c + half) ^ (col & 15)) * 16));
-    s = mma_32x32x16<DT>(a, q[c], s);
+    s[c & 1] = mma_32x32x16<DT>(a, q[c], s[c & 1]);
   }
-  return s;
+  return s[0] + s[1];
 }
 
 // How far a row is from key 0 of a lane's scores of the 32 keys from k0 on.  (Exact below 2^24 tokens; beyond, off by a part in 2^24.)
@@ -194,10 +199,13 @@ __device__ __forceinline__ float new_maximum(const AttendParams& p, float mx, St
     rarely();
     const float mn = rises ? mx : st.m;
     const float alpha = rises ? exp2_fast(st.m - mn) : 1.0f;
+    const bool some = __any(st.m != -__builtin_inff());  // (else the output is still zero)
     st.m = mn;
     st.l *= alpha;
+    if (some) {
 #pragma unroll
-    for (int t = 0; t < 4; ++t) st.o[t] *= alpha;
+      for (int t = 0; t < 4; ++t) st.o[t] *= alpha;
+    }
   }
   return st.m == -__builtin_inff() ? 0.0f : st.m;  // nothing seen yet: weights 0, not NaN
 }
@@ -395,18 +403,27 @@ __device__ __forceinline__ void copies_but() { asm volatile("s_waitcnt vmcnt(%0)
 __device__ __forceinline__ void lds_read() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
 // The interval of a row, and the row itself: pair f = f0 + i of the tile.
-__device__ __forceinline__ RowOf row_of(const AttendParams& p, const Tile& t, bool shared, int own_from, int group, int kv_head, int64_t f) {
+// Which (token, query head of the group) pair i of a tile is: a division by the group size that a product does for i < 8192.
+struct PairOf {
+  int tok, g;
+};
+__device__ __forceinline__ PairOf pair_of_tile(const AttendParams& p, const Tile& t, int i) {
+  const int x = t.g0 + i, tok = (x * p.inv_G) >> 16;
+  return PairOf{t.tok0 + tok, x - tok * p.G};
+}
+__device__ __forceinline__ RowOf row_of(const AttendParams& p, const Tile& t, bool shared, int own_from, int group, int kv_head, int i) {
   RowOf r;
   r.row = -1;
   r.head = kv_head * p.G;
   r.pos = 0;
   r.lo = 0;
   r.hi = -1;
-  if (f >= (int64_t)t.n * p.G) return r;
-  const int tok = (int)((uint64_t)f / (uint32_t)p.G), g = (int)(f - (int64_t)tok * p.G);
+  if (i >= t.pairs) return r;
+  const PairOf pair = pair_of_tile(p, t, i);
+  const int tok = pair.tok;
   r.row = t.r0 + tok;
-  r.head += g;
-  int b = t.table_row;
+  r.head += pair.g;
+  const int b = t.table_row;
   if (shared) {
     r.hi = t.limit - 1;
     if (p.window || p.slopes) {  // the request that the row belongs to
@@ -428,7 +445,9 @@ __device__ __forceinline__ RowOf row_of(const AttendParams& p, const Tile& t, bo
   return r;
 }
 
-constexpr int ATT_LDS = 65536;  // wide: a block of 64 keys, twice; narrow: 32 keys a wave, and later the waves' outputs
+// Wide: a block of 64 keys, twice.  Narrow: 32 keys a wave, and later the waves' outputs, whose rows lie four banks apart.
+constexpr int NARROW_PITCH = ABSB_HEAD_DIM + 4, ATT_LDS = ATT_WAVES * 32 * NARROW_PITCH * 4;
+static_assert(ATT_LDS >= 65536 && 2 * (ATT_LDS + 2048) <= 160 * 1024, "two work-groups a compute unit");
 
 template <int DT, int CAP, bool BIAS>
 __global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) {
@@ -436,6 +455,7 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) 
   __shared__ float s_ml[ATT_WAVES][2][32];
   __shared__ int s_lo[ATT_WAVES], s_hi[ATT_WAVES];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  fetch_arguments<0, sizeof(AttendParams)>();  // (what follows is a chain of round trips; the arguments make one of it)
 
   // ---- which phase, tile, KV head and split: heads go round the dies first, so that a head's keys stay in one die's L2 where
   // there are eight; long tiles (prefixes, the last ones of a causal prompt) start first
@@ -449,18 +469,28 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) 
   const uint32_t rest = unit / (uint32_t)p.Hkv;
   const int split = (int)(rest % (uint32_t)splits);
   const int64_t slot = ph.slots - 1 - (int64_t)(rest / (uint32_t)splits);
-  const Owner own = owner_of(owners, slot, p.G, log2_tile, [&](int o) { return p.row_off[shared ? p.first[o] : o]; });
+  int group_first = 0, group_len = 0;
+  if (!shared && p.groups) {
+    const int mine = min(lane, p.groups - 1);
+    group_first = p.first[mine];
+    group_len = p.len[mine];
+  }
+  const Owner own = owner_of(owners, slot, p.G, log2_tile, shared ? p.len : p.seq_lens, [&](int o) { return p.row_off[shared ? p.first[o] : o]; });
   const int owner = own.o;
   Tile t;
   t.r0 = own.r0;
   t.n = own.r1 - own.r0;
-  t.f0 = (slot - (((int64_t)t.r0 * p.G >> log2_tile) + owner)) << log2_tile;
-  if (t.f0 >= (int64_t)t.n * p.G) return;
+  // (an owner's pairs are fewer than 2^31: absb_attend_* sees to it)
+  const uint32_t f0 = (uint32_t)(slot - (((int64_t)t.r0 * p.G >> log2_tile) + owner)) << log2_tile;
+  t.pairs = (int)((uint32_t)t.n * (uint32_t)p.G - f0);
+  if (t.pairs <= 0) return;
+  t.tok0 = (int)(f0 / (uint32_t)p.G);
+  t.g0 = (int)(f0 - (uint32_t)t.tok0 * p.G);
   t.table_row = shared ? p.first[owner] : owner;
-  t.limit = shared ? p.len[owner] : p.seq_lens[owner];
-  const int own_from = !shared && p.groups ? shared_tokens(p, owner) : 0;
+  t.limit = own.len;
+  const int own_from = !shared && p.groups ? shared_tokens(p, owner, group_first, group_len) : 0;
 
-  const RowOf row = row_of(p, t, shared, own_from, owner, kv_head, t.f0 + (wide ? 32 * wave : 0) + (lane & 31));
+  const RowOf row = row_of(p, t, shared, own_from, owner, kv_head, (wide ? 32 * wave : 0) + (lane & 31));
   const bool valid = row.row >= 0, sees = valid && row.lo <= row.hi;
   const int lo = sees ? row.lo : INT32_MAX, hi = sees ? row.hi : -1;
   auto lesser = [](uint32_t a, uint32_t b) { return a < b ? a : b; };
@@ -622,11 +652,38 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) 
   }
   st.l = across_halves(st.l, [](float a, float b) { return a + b; });
 
-  // ---- the waves of a narrow tile have keys of their own: their states become one, a quarter of the channels a wave
-  if (!wide) {
-    __syncthreads();
-    float* s_o = reinterpret_cast<float*>(s_kv);  // [wave][channel][row]
-    const int half = lane >> 5, col = lane & 31;
+  const bool one = p.parts == 1, none = !one && begin >= end;  // (a split without keys has weight 0: its sum says so)
+  const int half = lane >> 5;
+  auto put_sums = [&](int64_t at, float m, float l) __attribute__((always_inline)) {
+    if (!one)
+      *reinterpret_cast<float2*>(p.part_ml + (at * p.parts + part0 + split) * 2) = make_float2(m, l);
+    else if (p.lse)
+      p.lse[at] = l > 0.0f ? (m + __builtin_log2f(l)) * LN2 : -__builtin_inff();
+  };
+  auto put = [&](int64_t at, int ch, f32x4 o, float inv) __attribute__((always_inline)) {
+    if (one)
+      *reinterpret_cast<uint2*>(p.out + at * ABSB_HEAD_DIM + ch) = uint2{pack2<DT>(o[0] * inv, o[1] * inv), pack2<DT>(o[2] * inv, o[3] * inv)};
+    else
+      *reinterpret_cast<f32x4*>(p.part_o + (at * p.parts + part0 + split) * ABSB_HEAD_DIM + ch) = o;
+  };
+  if (wide) {
+    if (!valid) return;
+    const int64_t at = (int64_t)row.row * p.Hq + row.head;
+    const float inv = st.l > 0.0f ? 1.0f / st.l : 0.0f;
+    if (half == 0) put_sums(at, st.m, st.l);
+    if (none) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)  // channels 32 i + 8 j + 4 half + 0 .. 3
+        put(at, 32 * i + 8 * j + 4 * half, f32x4{st.o[i][4 * j], st.o[i][4 * j + 1], st.o[i][4 * j + 2], st.o[i][4 * j + 3]}, inv);
+    return;
+  }
+  // The waves of a narrow tile have keys of their own: their states become one, eight threads a row.
+  __syncthreads();
+  float* s_o = reinterpret_cast<float*>(s_kv);  // [wave][row][channel], rows NARROW_PITCH apart
+  if (valid) {
+    const int col = lane & 31;
     if (half == 0) {
       s_ml[wave][0][col] = st.m;
       s_ml[wave][1][col] = st.l;
@@ -634,58 +691,34 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) 
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int j = 0; j < 16; ++j) s_o[wave * 4096 + (32 * i + 8 * (j >> 2) + 4 * half + (j & 3)) * 32 + col] = st.o[i][j];
-    __syncthreads();
-    float m = -__builtin_inff(), w[ATT_WAVES];
-#pragma unroll
-    for (int x = 0; x < ATT_WAVES; ++x) m = fmaxf(m, s_ml[x][0][col]);
-    const float base = m == -__builtin_inff() ? 0.0f : m;
-    float l = 0.0f;
-#pragma unroll
-    for (int x = 0; x < ATT_WAVES; ++x) {
-      w[x] = exp2_fast(s_ml[x][0][col] - base);
-      l = __builtin_fmaf(s_ml[x][1][col], w[x], l);
-    }
-    st.m = m;
-    st.l = l;
-#pragma unroll
-    for (int j = 0; j < 16; ++j) {
-      const int at = (32 * wave + 8 * (j >> 2) + 4 * half + (j & 3)) * 32 + col;
-      float v = 0.0f;
-#pragma unroll
-      for (int x = 0; x < ATT_WAVES; ++x) v = __builtin_fmaf(s_o[x * 4096 + at], w[x], v);
-      st.o[0][j] = v;
-    }
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<f32x4*>(s_o + (wave * 32 + col) * NARROW_PITCH + 32 * i + 8 * j + 4 * half) =
+            f32x4{st.o[i][4 * j], st.o[i][4 * j + 1], st.o[i][4 * j + 2], st.o[i][4 * j + 3]};
   }
-  if (!valid) return;
-
-  // ---- out: channels 32 t + 8 (i / 4) + 4 half + i % 4, four at a time (narrow: the wave's 32, in o[0])
-  const int half = lane >> 5;
-  const int64_t at = (int64_t)row.row * p.Hq + row.head;
-  const bool one = p.parts == 1;
-  const int64_t part = at * p.parts + part0 + split;
-  const float inv = st.l > 0.0f ? 1.0f / st.l : 0.0f;
-  if (half == 0 && (wide || wave == 0)) {
-    if (!one)
-      *reinterpret_cast<float2*>(p.part_ml + part * 2) = make_float2(st.m, st.l);
-    else if (p.lse)
-      p.lse[at] = st.l > 0.0f ? (st.m + __builtin_log2f(st.l)) * LN2 : -__builtin_inff();
+  __syncthreads();
+  const int r = (int)threadIdx.x >> 3, c = (int)threadIdx.x & 7;
+  if (r >= t.pairs) return;
+  const PairOf pair = pair_of_tile(p, t, r);
+  const int64_t at = (int64_t)(t.r0 + pair.tok) * p.Hq + kv_head * p.G + pair.g;
+  float m = -__builtin_inff(), l = 0.0f, w[ATT_WAVES];
+#pragma unroll
+  for (int x = 0; x < ATT_WAVES; ++x) m = fmaxf(m, s_ml[x][0][r]);
+  const float base = m == -__builtin_inff() ? 0.0f : m;
+#pragma unroll
+  for (int x = 0; x < ATT_WAVES; ++x) {
+    w[x] = exp2_fast(s_ml[x][0][r] - base);
+    l = __builtin_fmaf(s_ml[x][1][r], w[x], l);
   }
-  if (!one && begin >= end) return;  // (a split without keys has weight 0: its sum says so)
-  auto put = [&](int ch, float a, float b, float c, float d) __attribute__((always_inline)) {
-    if (one) {
-      const uint2 w = {pack2<DT>(a * inv, b * inv), pack2<DT>(c * inv, d * inv)};
-      *reinterpret_cast<uint2*>(p.out + at * ABSB_HEAD_DIM + ch) = w;
-    } else {
-      *reinterpret_cast<f32x4*>(p.part_o + part * ABSB_HEAD_DIM + ch) = f32x4{a, b, c, d};
-    }
-  };
+  if (c == 0) put_sums(at, m, l);
+  if (none) return;
+  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (!wide && i > 0) break;
+  for (int j = 0; j < 4; ++j) {
+    const int ch = 32 * j + 4 * c;
+    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      put(32 * (wide ? i : wave) + 8 * j + 4 * half, st.o[i][4 * j], st.o[i][4 * j + 1], st.o[i][4 * j + 2], st.o[i][4 * j + 3]);
+    for (int x = 0; x < ATT_WAVES; ++x) o += *reinterpret_cast<const f32x4*>(s_o + (x * 32 + r) * NARROW_PITCH + ch) * w[x];
+    put(at, ch, o, inv);
   }
 }
 
