@@ -394,7 +394,7 @@ ABSB_API int absb_assign_block_sizes(int32_t n_samples, int32_t n_heads, int32_t
  * everything their requests hold, on the same paged caches and page tables as the rest of the library.
  * They read layer->num_q_heads, num_kv_heads, head_dim, page_size, dtype, the K/V strides (kv_stride_tok
  * at most 2^28) and sm_scale; block sizes and the selection policy do not matter to them
- * (layer->block_size may be NULL).  Lengths may be 0 here.
+ * (layer->block_size may be NULL).  Lengths may be 0 here, and at most 2^30; rows times query heads stay below 2^31.
  *
  * "Rows": the new tokens of all requests side by side, request b's at [row_off[b], row_off[b+1]).  They
  * are the LAST tokens of their context: with n_b rows and length L_b (which counts them), row
@@ -430,7 +430,7 @@ typedef struct absb_page_ring {
  * All or nothing: if the ring holds too few free pages, or a table row is too short for its request's
  * pages, then no table, no page and no cursor changes, every row_slot is -1 and cursors_out[2] (written
  * with a ring only) says how many pages were missing.  Without a ring, rows beyond the table's width get
- * slot -1.  Sums of rows and of pages must stay below 2^31; batch is at most 65535.  Reads batch->batch,
+ * slot -1.  max_rows is at most 2^30, batch at most 65535; sums of rows and of pages must stay below 2^31.  Reads batch->batch,
  * pt_stride and seq_lens, and layer->page_size. */
 ABSB_API int absb_map_rows(const absb_layer* layer, const absb_batch* batch, const int32_t* lens_before,
                            int32_t* page_table, const absb_page_ring* ring, int32_t max_rows, int32_t* row_off,
@@ -487,7 +487,7 @@ ABSB_API int absb_rotate_store(const absb_layer* layer, const absb_rope* rope, i
  * score = sm_scale * q.k;  then softcap * tanh(score / softcap) (if set);  then - slopes[head] * |i - j| (if
  * set).  All zero and NULL: causal attention.  A row that sees nothing yields out = 0, lse = -inf. */
 typedef struct absb_score_opts {
-  float softcap;              /* 0 = none, else > 0                                              */
+  float softcap;              /* 0 = none, else 1e-30 to 1e30                                    */
   int32_t window;             /* 0 = none, else >= 1: tokens a row sees up to and including itself      */
   const float* slopes;        /* device [Hq] or NULL                                             */
   const int32_t* prefix_lens; /* device [Bt] or NULL: tokens that all rows of a request see            */

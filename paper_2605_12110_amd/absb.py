@@ -319,8 +319,9 @@ _BATCH_FIELDS = (*_BATCH_HOST_ARRAYS, *_BATCH_TENSORS, "pt_stride")
 
 
 class _Record:
-    """Host description whose C record is built once per set of field values (any assignment drops it).  Tensors are
-    held by address: one that is resized in place has to be assigned again."""
+    """Host description whose C record is built once per set of field values (any assignment drops it).  What it was made from
+    in place of an int32 array (a list, say) has been copied, and tensors are held by address: one that is changed in
+    place, or resized, has to be assigned again."""
 
     def __setattr__(self, name, value):
         object.__setattr__(self, name, value)
@@ -587,9 +588,16 @@ def absb_attend_workspace(layer: Layer, batch: Batch, rows: Rows, shared: Shared
     return int(n.value)
 
 
+def _dense(where: str, *tensors) -> None:
+    for t in tensors:
+        if t is not None and t.__class__ is not int and not t.is_contiguous():
+            raise AbsbError(ERR_BAD_SHAPE, where)
+
+
 def absb_attend_rows(layer: Layer, batch: Batch, rows: Rows, q, k_cache, v_cache, out, lse=None, opts: ScoreOpts = None,
                      workspace=None, stream=None) -> None:
     cl, cb = layer.c(), batch.c()
+    _dense("absb_attend_rows", q, out)
     _check(load().absb_attend_rows(C.byref(cl), C.byref(cb), _rec(rows), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(out), _ptr(lse),
                                    _rec(opts), _ptr(workspace), _nbytes(workspace), _stream(stream)), "absb_attend_rows")
 
@@ -597,6 +605,7 @@ def absb_attend_rows(layer: Layer, batch: Batch, rows: Rows, q, k_cache, v_cache
 def absb_attend_shared(layer: Layer, batch: Batch, rows: Rows, shared: SharedPrefix, q, k_cache, v_cache, out, lse=None,
                        opts: ScoreOpts = None, workspace=None, stream=None) -> None:
     cl, cb = layer.c(), batch.c()
+    _dense("absb_attend_shared", q, out)
     _check(load().absb_attend_shared(C.byref(cl), C.byref(cb), _rec(rows), _rec(shared), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(out),
                                      _ptr(lse), _rec(opts), _ptr(workspace), _nbytes(workspace), _stream(stream)), "absb_attend_shared")
 

@@ -388,7 +388,7 @@ static int plan_attend(const absb_layer* layer, const absb_batch* batch, const a
   if (off[0] != 0) return ABSB_ERR_BAD_SHAPE;
   int64_t max_len = 0, max_n = 0;
   for (int b = 0; b < Bt; ++b) {
-    if (off[b + 1] < off[b] || off[b + 1] - off[b] > lens[b]) return ABSB_ERR_BAD_SHAPE;
+    if (off[b + 1] < off[b] || off[b + 1] - off[b] > lens[b] || lens[b] > (1 << 30)) return ABSB_ERR_BAD_SHAPE;
     max_len = std::max<int64_t>(max_len, lens[b]);
     max_n = std::max<int64_t>(max_n, off[b + 1] - off[b]);
   }
@@ -743,7 +743,8 @@ int absb_map_rows(const absb_layer* layer, const absb_batch* batch, const int32_
   if (!layer || !batch) return ABSB_ERR_NULL;
   const int P = layer->page_size;
   if (!is_pow2(P) || P < 8 || P > 65536) return ABSB_ERR_BAD_SHAPE;
-  if (batch->batch < 1 || batch->batch > 65535 || batch->pt_stride < 0 || max_rows < 0) return ABSB_ERR_BAD_SHAPE;
+  if (batch->batch < 1 || batch->batch > 65535 || batch->pt_stride < 0 || max_rows < 0 || max_rows > (1 << 30))
+    return ABSB_ERR_BAD_SHAPE;
   if (!lens_before || !batch->seq_lens || !row_off || (!page_table && batch->pt_stride)) return ABSB_ERR_NULL;
   if (max_rows && (!row_pos || !row_slot)) return ABSB_ERR_NULL;
   if (ring) {
@@ -865,7 +866,8 @@ static int attend(const absb_layer* layer, const absb_batch* batch, const absb_r
                   const void* q, const void* k_cache, const void* v_cache, void* out, float* lse,
                   const absb_score_opts* opts, void* workspace, size_t workspace_bytes, void* stream) {
   const float cap = opts ? opts->softcap : 0.0f;
-  if (!(cap >= 0.0f) || std::isinf(cap) || (opts && opts->window < 0)) return ABSB_ERR_BAD_SHAPE;
+  // (beyond these a factor of the cap overflows binary32)
+  if (!(cap == 0.0f || (cap >= 1e-30f && cap <= 1e30f)) || (opts && opts->window < 0)) return ABSB_ERR_BAD_SHAPE;
   AttendPlan plan;
   int rc = plan_attend(layer, batch, rows, shared, opts, false, &plan);
   if (rc != ABSB_OK) return rc;

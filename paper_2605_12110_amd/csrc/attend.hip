@@ -70,12 +70,12 @@ __device__ __forceinline__ Owner owner_of(int n, int64_t x, int G, int log2_tile
   while (hi - lo > 63) {
     const int step = (hi - lo + 63) >> 6, at = lo + lane * step;
     const uint64_t below = __ballot(at < hi && (((int64_t)row0(min(at, hi - 1)) * G) >> log2_tile) + at <= x);
-    lo += (__popcll(below) - 1) * step;
+    lo += max(0, __popcll(below) - 1) * step;
     hi = min(hi, lo + step);
   }
   const int at = min(lo + lane, hi), r = row0(at), len = lens[min(at, n - 1)];
   const uint64_t below = __ballot(lo + lane < hi && (((int64_t)r * G) >> log2_tile) + at <= x);
-  const int i = __popcll(below) - 1;
+  const int i = max(0, __popcll(below) - 1);
   return Owner{lo + i, __builtin_amdgcn_readlane(r, i), __builtin_amdgcn_readlane(r, i + 1), __builtin_amdgcn_readlane(len, i)};
 }
 // The shared tokens of request b: those of the last group g with first[g] <= b.  `first`, `len`: the lane's group of the first 64,
@@ -85,7 +85,7 @@ __device__ __forceinline__ int shared_tokens(const AttendParams& p, int b, int f
   int lo = 0, hi = p.groups;
   while (hi - lo > 64) {
     const int step = (hi - lo + 63) >> 6, at = lo + lane * step;
-    lo += (__popcll(__ballot(at < hi && p.first[min(at, hi - 1)] <= b)) - 1) * step;
+    lo += max(0, __popcll(__ballot(at < hi && p.first[min(at, hi - 1)] <= b)) - 1) * step;
     hi = min(hi, lo + step);
     if (hi - lo <= 64) {
       const int mine = min(lo + lane, hi - 1);
@@ -93,7 +93,7 @@ __device__ __forceinline__ int shared_tokens(const AttendParams& p, int b, int f
       len = p.len[mine];
     }
   }
-  return __builtin_amdgcn_readlane(len, __popcll(__ballot(lo + lane < hi && first <= b)) - 1);
+  return __builtin_amdgcn_readlane(len, max(0, __popcll(__ballot(lo + lane < hi && first <= b)) - 1));
 }
 
 struct RowOf {
@@ -404,7 +404,6 @@ __device__ __forceinline__ void copies_but() { asm volatile("s_waitcnt vmcnt(%0)
 // What the wave read of LDS has arrived: a copy may take its place.
 __device__ __forceinline__ void lds_read() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
-// The interval of a row, and the row itself: pair f = f0 + i of the tile.
 // Which (token, query head of the group) pair i of a tile is: a division by the group size that a product does for i < 8192.
 struct PairOf {
   int tok, g;
@@ -413,6 +412,7 @@ __device__ __forceinline__ PairOf pair_of_tile(const AttendParams& p, const Tile
   const int x = t.g0 + i, tok = (x * p.inv_G) >> 16;
   return PairOf{t.tok0 + tok, x - tok * p.G};
 }
+// Pair i of a tile, and the interval of keys that it sees.
 __device__ __forceinline__ RowOf row_of(const AttendParams& p, const Tile& t, bool shared, int own_from, int group, int kv_head, int i) {
   RowOf r;
   r.row = -1;
@@ -660,7 +660,7 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) 
     if (!one)
       *reinterpret_cast<float2*>(p.part_ml + (at * p.parts + part0 + split) * 2) = make_float2(m, l);
     else if (p.lse)
-      p.lse[at] = l > 0.0f ? (m + __builtin_log2f(l)) * LN2 : -__builtin_inff();
+      p.lse[at] = l == 0.0f ? -__builtin_inff() : (m + __builtin_log2f(l)) * LN2;
   };
   auto put = [&](int64_t at, int ch, f32x4 o, float inv) __attribute__((always_inline)) {
     if (one)
@@ -671,7 +671,7 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) 
   if (wide) {
     if (!valid) return;
     const int64_t at = (int64_t)row.row * p.Hq + row.head;
-    const float inv = st.l > 0.0f ? 1.0f / st.l : 0.0f;
+    const float inv = st.l == 0.0f ? 0.0f : 1.0f / st.l;
     if (half == 0) put_sums(at, st.m, st.l);
     if (none) return;
 #pragma unroll
@@ -713,7 +713,7 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) 
   }
   if (c == 0) put_sums(at, m, l);
   if (none) return;
-  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const int ch = 32 * j + 4 * c;
@@ -738,7 +738,7 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(AttendParams p, int64
   for (int i0 = 0; i0 < p.parts; i0 += 64) {
     float2 mine = make_float2(-__builtin_inff(), 0.0f);
     if (i0 + lane < p.parts) mine = *reinterpret_cast<const float2*>(ml + (i0 + lane) * 2);
-    if (!(mine.y > 0.0f)) mine = make_float2(-__builtin_inff(), 0.0f);
+    if (mine.y == 0.0f) mine.x = -__builtin_inff();  // (a NaN stays one)
     const float top = fmaxf(M, wave_max_f32(mine.x)), base = top == -__builtin_inff() ? 0.0f : top;
     const float a = exp2_fast(M - base), w = exp2_fast(mine.x - base);
     M = top;
@@ -762,10 +762,10 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(AttendParams p, int64
   L = row16_sum(L);
   L = bitcast<float>(__builtin_amdgcn_readlane(bitcast<int>(L), 0)) + bitcast<float>(__builtin_amdgcn_readlane(bitcast<int>(L), 16)) +
       bitcast<float>(__builtin_amdgcn_readlane(bitcast<int>(L), 32)) + bitcast<float>(__builtin_amdgcn_readlane(bitcast<int>(L), 48));
-  const float inv = L > 0.0f ? 1.0f / L : 0.0f;
+  const float inv = L == 0.0f ? 0.0f : 1.0f / L;
   if (half == 0)
     *reinterpret_cast<uint2*>(p.out + at * ABSB_HEAD_DIM + 4 * lane) = uint2{pack2<DT>(x[0] * inv, x[1] * inv), pack2<DT>(x[2] * inv, x[3] * inv)};
-  if (p.lse && lane == 0) p.lse[at] = L > 0.0f ? (M + __builtin_log2f(L)) * LN2 : -__builtin_inff();
+  if (p.lse && lane == 0) p.lse[at] = L == 0.0f ? -__builtin_inff() : (M + __builtin_log2f(L)) * LN2;
 }
 
 template <int DT, int CAP, bool BIAS>

@@ -164,10 +164,12 @@ __global__ __launch_bounds__(T) void map_rows_kernel(MapParams p) {
 }
 
 int launch_map_rows(const MapParams& p, hipStream_t stream) {
-  // a row or two a thread, at most a work-group a compute unit
+  // a row or two a thread; with a ring, a work-group for every 128 requests, whose pages the host does not know; at most one a
+  // compute unit (a second one costs a decode step 1 us: the cursors wait for both)
   const int threads = p.batch <= 256 ? 256 : p.batch <= 512 ? 512 : 1024;
-  const int wgs = p.max_rows <= 2 * threads ? 1 : p.max_rows / threads;
-  const int grid = wgs < 256 ? wgs : 256;
+  const int by_rows = p.max_rows <= 2 * threads ? 1 : p.max_rows / threads, by_pages = p.ring ? p.batch / 128 : 1;
+  const int wgs = by_rows > by_pages ? by_rows : by_pages;
+  const int grid = wgs < 1 ? 1 : wgs < 256 ? wgs : 256;
   if (threads == 256)
     hipLaunchKernelGGL((map_rows_kernel<256>), dim3(grid), dim3(256), 0, stream, p);
   else if (threads == 512)

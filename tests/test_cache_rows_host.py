@@ -117,6 +117,7 @@ def test_map_rows_refusals():
     _refused(absb.ERR_NULL, f, *_map(off=None))
     _refused(absb.ERR_NULL, f, *_map(pos=_T(4, at=None)))
     _refused(absb.ERR_BAD_SHAPE, f, *_map(pos=_T(5)))
+    _refused(absb.ERR_BAD_SHAPE, f, *_map(pos=_T((1 << 30) + 1), slot=_T((1 << 30) + 1)))
     _refused(absb.ERR_NULL, f, *_map(batch=absb.Batch(seq_lens_host=[5], pt_stride=1)))
     _refused(absb.ERR_BAD_SHAPE, f, *_map(batch=_batch([1] * 65536)))
     _refused(absb.ERR_BAD_SHAPE, f, *_map(batch=_batch([5], width=-1)))
@@ -172,7 +173,11 @@ BIG_WS = _T(1 << 40, size=1)
     (dict(q=None), absb.ERR_NULL), (dict(k=None), absb.ERR_NULL), (dict(v=None), absb.ERR_NULL), (dict(out=None), absb.ERR_NULL),
     (dict(q=AT + 8), absb.ERR_BAD_SHAPE), (dict(out=AT + 2), absb.ERR_BAD_SHAPE), (dict(k=AT + 4), absb.ERR_BAD_SHAPE),
     (dict(opts=absb.ScoreOpts(softcap=-1.0)), absb.ERR_BAD_SHAPE), (dict(opts=absb.ScoreOpts(softcap=math.nan)), absb.ERR_BAD_SHAPE),
-    (dict(opts=absb.ScoreOpts(softcap=math.inf)), absb.ERR_BAD_SHAPE), (dict(opts=absb.ScoreOpts(window=-1)), absb.ERR_BAD_SHAPE),
+    (dict(opts=absb.ScoreOpts(softcap=math.inf)), absb.ERR_BAD_SHAPE), (dict(opts=absb.ScoreOpts(softcap=1e-31)), absb.ERR_BAD_SHAPE),
+    (dict(opts=absb.ScoreOpts(softcap=1e31)), absb.ERR_BAD_SHAPE), (dict(q=_T(3, 32, D, stride0=48 * D)), absb.ERR_BAD_SHAPE),
+    (dict(out=_T(3, 32, D, stride0=48 * D)), absb.ERR_BAD_SHAPE), (dict(lens=(100, (1 << 30) + 1)), absb.ERR_BAD_SHAPE),
+    (dict(lens=(1 << 27, 5), new=(1 << 27, 1)), absb.ERR_BAD_SHAPE),          # 2^32 pairs of row and head
+    (dict(opts=absb.ScoreOpts(window=-1)), absb.ERR_BAD_SHAPE),
     (dict(lens=(5000, 9000)), absb.ERR_WORKSPACE), (dict(lens=(5000, 9000), ws=_T(100, size=1)), absb.ERR_WORKSPACE),
     (dict(lens=(5000, 9000), ws=_T(1 << 40, at=AT + 16, size=1)), absb.ERR_WORKSPACE),
 ])

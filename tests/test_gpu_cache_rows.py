@@ -155,6 +155,11 @@ def test_map_rows_all_or_nothing_when_pages_or_places_are_missing():
     assert want[2].count(-1) == 4
 
 
+def test_map_rows_when_many_pages_come_back():
+    _map_case([9000] * 300, [0] * 300, 8)
+    _map_case([900] * 2000 + [3], [0] * 2000 + [9], 8, in_place=False)
+
+
 def test_map_rows_pads_and_cuts_at_max_rows():
     _map_case([3, 0], [9, 30], 8, max_rows=50)
     _map_case([3, 0], [9, 30], 8, max_rows=10)
@@ -495,6 +500,110 @@ def test_attend_shared_masks():
     docs = np.array([0, 100, 64, 63, 128, 2 ** 31 - 1], np.int32)
     for kw in (dict(docs=docs), dict(prefix=[10, 200, 0]), dict(docs=docs, prefix=[132, 131, 130], window=90)):
         Call([130, 131, 132], [2, 1, 3], 8, 2, 16, "f16", shared=[64], **kw).check(str(kw.keys()))
+
+
+def test_attend_of_many_requests_and_groups():
+    """More owners than a wave looks at in one go: requests, and groups, some of them empty."""
+    r = np.random.default_rng(9)
+    for B, hi in ((64, 40), (65, 40), (200, 30), (4500, 9)):
+        lens = r.integers(0, hi, B)
+        Call(lens, np.minimum(lens, r.integers(0, 3, B)), 4, 2, 8, "f16", seed=B).check(f"{B} requests")
+    lens = r.integers(9, 30, 300)
+    first = np.sort(np.concatenate([[0, 300], r.integers(0, 301, 149)]))
+    Call(lens, np.ones(300, np.int64), 4, 2, 8, "f16", shared=(8 * r.integers(0, 2, 150)).tolist(), first=first.tolist(), slopes=True,
+         window=20).check("150 groups")
+    Call(lens, r.integers(0, 9, 300), 8, 1, 8, "bf16", shared=[0] * 74 + [8] + [0] * 75, first=first.tolist()).check("one group shares")
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(5, 1), (7, 1), (3, 1), (8, 1), (1, 1)])
+def test_attend_windows_over_splits_of_odd_groups(Hq, Hkv):
+    for window in (1, 63, 64, 65, 127, 700, 1500):
+        Call([9001], [130], Hq, Hkv, 16, "f16", window=window).check(f"chunk, window {window}, {Hq} heads")
+        Call([9001, 333], [1, 2], Hq, Hkv, 16, "f16", window=window).check(f"tokens, window {window}, {Hq} heads")
+
+
+def test_attend_of_more_than_64_parts():
+    absb = _absb()
+    c = Call([120001], [1], 8, 1, 64, "f16", shared=[60032])
+    assert absb.absb_attend_workspace(c.layer, c.batch, c.r, c.shared) > 64 * 8 * 520
+    c.check("prefix and own keys of 60 K")
+
+
+def test_attend_rows_of_nan_keep_to_themselves():
+    torch = _torch()
+    for lens, new in (([300], [200]), ([5000], [2]), ([40], [3])):
+        c = Call(lens, new)
+        c.run()
+        torch.cuda.synchronize()
+        want, want_lse = c.out[:c.rows].clone(), c.lse[:c.rows].clone()
+        c.q[1] = float("nan")
+        c.run()
+        torch.cuda.synchronize()
+        others = [i for i in range(c.rows) if i != 1]
+        assert torch.equal(c.out[others], want[others]) and torch.equal(c.lse[others], want_lse[others])
+        assert torch.isnan(c.out[1]).all()
+
+
+def test_attend_without_log_sums():
+    torch, absb = _torch(), _absb()
+    for c in (Call([600], [200]), Call([9000], [1]), Call([40], [1])):
+        c.run()
+        torch.cuda.synchronize()
+        want = c.out.clone()
+        c.out.fill_(0)
+        absb.absb_attend_rows(c.layer, c.batch, c.r, c.q, c.k, c.v, c.out, None, c.opts, c.ws)
+        torch.cuda.synchronize()
+        assert torch.equal(c.out[:c.rows], want[:c.rows])
+
+
+def test_attend_and_rotate_beyond_4_gib_of_cache():
+    """Pages whose offsets pass 32 bits, in bytes and in elements."""
+    torch, absb = _torch(), _absb()
+    P, Hkv, Hq = 64, 2, 8
+    lens, new = [700, 130], [3, 130]
+    c = Call(lens, new, Hq, Hkv, P)
+    c.run()
+    torch.cuda.synchronize()
+    want, want_lse = c.out[:c.rows].clone(), c.lse[:c.rows].clone()
+    pages = (9 << 30) // (Hkv * P * D * 2)
+    K, V = (torch.empty((pages, Hkv, P, D), dtype=torch.float16, device="cuda") for _ in range(2))
+    old = c.batch.page_table.clone()
+    used = old < c.k.shape[0]
+    table = torch.where(used, pages - 1 - old * (pages // (2 * c.k.shape[0])), old).int()
+    K[table[used].long()], V[table[used].long()] = c.k[old[used].long()], c.v[old[used].long()]
+    c.batch = absb.Batch(seq_lens_host=c.lens, seq_lens=c.batch.seq_lens, page_table=table)
+    c.k, c.v = K, V
+    c.run()
+    torch.cuda.synchronize()
+    assert torch.equal(c.out[:c.rows], want) and torch.equal(c.lse[:c.rows], want_lse)
+    n = 5
+    k, v = (torch.randn((n, Hkv, D), device="cuda").half() for _ in range(2))
+    slot = torch.tensor([0, pages * P - 1, pages * P // 2, pages * P // 3, -1], dtype=torch.int64, device="cuda")
+    freq = torch.zeros(64, dtype=torch.float64, device="cuda")
+    absb.absb_rotate_store(c.layer, absb.Rope(), torch.zeros(n, dtype=torch.int32, device="cuda"), slot, freq, k=k, v=v, k_cache=K, v_cache=V)
+    torch.cuda.synchronize()
+    page, at = slot[:4] // P, slot[:4] % P
+    assert torch.equal(K[page, :, at], k[:4]) and torch.equal(V[page, :, at], v[:4])
+
+
+def test_attend_of_tokens_half_a_gib_apart():
+    """The widest token stride: the last of eight rows is 3.5 GiB behind the first."""
+    torch, absb = _torch(), _absb()
+    step = 1 << 28
+    for n in (1, 8):
+        c = Call([8], [n], 4, 1, 8)
+        c.run()
+        torch.cuda.synchronize()
+        want, want_lse = c.out[:c.rows].clone(), c.lse[:c.rows].clone()
+        page = int(c.table_host[0, 0])
+        K, V = (torch.empty((8 * step,), dtype=torch.float16, device="cuda") for _ in range(2))
+        for t in range(8):
+            K[t * step:t * step + D], V[t * step:t * step + D] = c.k[page, 0, t], c.v[page, 0, t]
+        layer = absb.Layer(4, 1, D, 8, absb.F16, None, (8 * step, D, step))
+        batch = absb.Batch(seq_lens_host=c.lens, seq_lens=c.batch.seq_lens, page_table=torch.zeros((1, 1), dtype=torch.int32, device="cuda"))
+        absb.absb_attend_rows(layer, batch, c.r, c.q, K, V, c.out, c.lse, None, c.ws)
+        torch.cuda.synchronize()
+        assert torch.equal(c.out[:c.rows], want) and torch.equal(c.lse[:c.rows], want_lse)
 
 
 def test_attend_scales_and_out_of_place_widths():
