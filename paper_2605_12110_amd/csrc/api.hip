@@ -457,7 +457,7 @@ static int plan_attend(const absb_layer* layer, const absb_batch* batch, const a
       for (int i = 0; i < 2; ++i) ph[i] = cut_phase(s[i], tile[i], (int64_t)std::ceil(whole[i] / stretch - 1e-6), owners[i], slots[i]);
       if (ph[1].splits > most_splits) break;
       const double us = attend_us(s, ph, (double)p.rows * layer->num_q_heads, Hkv);
-      if (cuts > 1 && us >= best) continue;
+      if (cuts > 1 && us >= 0.98 * best) continue;  // (as good as level: fewer parts)
       best = us;
       p.shared = ph[0];
       p.own = ph[1];
