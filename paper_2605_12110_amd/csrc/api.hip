@@ -349,10 +349,10 @@ static AttendPhase cut_phase(const PhaseSums& s, int log2_tile, int64_t splits, 
 //   128-row tiles are bound by the matrix unit: a key takes a work-group 0.018 us alone on a compute unit, twice that as one of two
 //   (512 work-groups in all).  Equal ones go in rounds; others leave part of one running behind, hardly any if they start
 //   in falling order, as a causal prompt's do.
-//   32-row tiles are bound by memory, 5.4 TB/s, or, if they are few, by what one work-group can ask for: 0.0093 us a key.
+//   32-row tiles are bound by memory, 6.0 TB/s, or, if they are few, by what one work-group can ask for: 0.0093 us a key.
 //   The two share a launch well.  Partial results are written and read once; the merge is a launch of its own.
 static double attend_us(const PhaseSums (&s)[2], const AttendPhase (&ph)[2], double pairs, int Hkv) {
-  constexpr double PLACES = 512, KEY_ALONE = 0.018, KEY_PAIRED = 0.036, KEY_NARROW = 0.0093, BYTES_US = 5.4e6, START = 8, MERGE = 5;
+  constexpr double PLACES = 512, KEY_ALONE = 0.018, KEY_PAIRED = 0.036, KEY_NARROW = 0.0093, BYTES_US = 6.0e6, START = 8, MERGE = 5;
   const int parts = ph[0].splits + ph[1].splits;
   double wide = 0, narrow = 0, bytes = 0, units = 0;
   for (int i = 0; i < 2; ++i) {
@@ -480,6 +480,9 @@ static int plan_attend(const absb_layer* layer, const absb_batch* batch, const a
   p.parts = p.shared.splits + p.own.splits;
   const int ws_parts = any_options ? parts_any : p.parts;
   if (p.shared.slots * Hkv * p.shared.splits + p.own.slots * Hkv * p.own.splits >= (int64_t(1) << 31)) return ABSB_ERR_BAD_SHAPE;
+  // Narrow tiles read a row once; what the last-level cache could not keep for the next call anyway passes it by (one token behind
+  // 128 K 101 -> 88 us, 64 behind 2 K 95 -> 84, 64 behind 1 K, 134 MB, 50.3 -> 44.7).
+  p.stream_rows = (sums[0].owners_keys + sums[1].owners_keys) * Hkv * 4 * ABSB_HEAD_DIM >= 96.0 * (1 << 20);
   const int64_t pairs = p.rows * layer->num_q_heads;
   if (ws_parts > 1) {
     p.ws_part_ml = align256((size_t)pairs * ws_parts * ABSB_HEAD_DIM * 4);
@@ -911,6 +914,7 @@ static int attend(const absb_layer* layer, const absb_batch* batch, const absb_r
   p.inv_G = (65536 + p.G - 1) / p.G;
   p.log2_page = ilog2(layer->page_size);
   p.parts = plan.parts;
+  p.stream_rows = plan.stream_rows;
   p.shared = plan.shared;
   p.own = plan.own;
   p.shared_units = (uint32_t)(plan.shared.slots * p.Hkv * plan.shared.splits);

@@ -20,6 +20,7 @@ struct AttendPlan {
   AttendPhase shared, own;  // shared.owners = 0: no such phase
   int32_t parts;            // partial results of a row: shared.splits + own.splits
   int64_t rows;
+  int32_t stream_rows;
   size_t ws_part_ml, ws_bytes;  // ws_bytes = 0: one part, written straight to the output
 };
 
@@ -38,6 +39,7 @@ struct AttendParams {
   int32_t batch, groups, pt_stride, Hq, Hkv, G, log2_page;
   int32_t inv_G;                  // 2^16 / G, rounded up
   int32_t window, parts;
+  int32_t stream_rows;            // 1: narrow tiles read rows past the caches
   float scale_log2;               // sm_scale * log2(e)
   float cap_log2, cap_in;         // cap * log2(e), 2 log2(e) sm_scale / cap (capped only)
   uint32_t shared_units;          // work-groups of the first phase, ahead of the second's

@@ -348,8 +348,12 @@ __device__ __forceinline__ Stretch stretch_on(const AttendParams& p, int32_t pag
 // compiler would wait for every copy in flight ahead of every read of LDS, the one of the next block included.  (It must wait
 // for none: copies_done() does, in front of the barrier behind which a block is read.  The waits: m0 wants one state ahead of the
 // copy, a scalar that came from a vector instruction five.)
+template <bool STREAM>  // past the caches
 __device__ __forceinline__ void copy_to_lds(const char* base, uint32_t lane_off, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(lane_off), "s"(base) : "memory");
+  if (STREAM)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(to), "v"(lane_off), "s"(base) : "memory");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(lane_off), "s"(base) : "memory");
 }
 __device__ __forceinline__ uint32_t lds_address(const char* at) {
   typedef __attribute__((address_space(3))) const char* lds;
@@ -378,14 +382,14 @@ struct Groups {
   bool full;
 };
 // Copies them from K or V to LDS, 2 N copies; rows that do not exist are the last that does again, which no one sees.
-template <bool KEY, int N>
+template <bool KEY, bool STREAM, int N>
 __device__ __forceinline__ void copy_groups(const char* base, const Groups<N>& g, uint32_t pitch, const LaneCopy& lc, uint32_t to) {
   auto copy = [&](auto all) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < 2 * N; ++j) {
       uint32_t at = KEY ? lc.key[j & 3] : lc.value[j & 1];
       if (!decltype(all)::value) at -= (uint32_t)max(0, 4 * (j & 1) + (int)((threadIdx.x & 63) >> 4) - g.most[j >> 1]) * pitch;
-      copy_to_lds(base + g.off[j >> 1], at, to + 4 * j * ROW_BYTES);
+      copy_to_lds<STREAM>(base + g.off[j >> 1], at, to + 4 * j * ROW_BYTES);
     }
   };
   if (g.full) {
@@ -558,8 +562,8 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) 
       const int steps = (end - begin + STEP - 1) / STEP;
       const char* mine = s_kv;
       const uint32_t to = lds_address(s_kv) + 16 * wave * ROW_BYTES;
-      auto copy_k = [&](const Groups<2>& g, int i) __attribute__((always_inline)) { copy_groups<true>(kb, g, pitch, lc, to + (i & 1) * STAGE); };
-      auto copy_v = [&](const Groups<2>& g, int i) __attribute__((always_inline)) { copy_groups<false>(vb, g, pitch, lc, to + (2 + (i & 1)) * STAGE); };
+      auto copy_k = [&](const Groups<2>& g, int i) __attribute__((always_inline)) { copy_groups<true, false>(kb, g, pitch, lc, to + (i & 1) * STAGE); };
+      auto copy_v = [&](const Groups<2>& g, int i) __attribute__((always_inline)) { copy_groups<false, false>(vb, g, pitch, lc, to + (2 + (i & 1)) * STAGE); };
       auto rows_of = [&](int i) __attribute__((always_inline)) { return groups(at, (i % PER) * 8 + 2 * wave, std::integral_constant<int, 2>()); };
       Groups<2> rows = rows_of(0);
       // Step i: the scores of block i + 1 are worked out beside the softmax of block i, matrix and vector unit at once; so K is
@@ -613,9 +617,22 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) 
       const char *kl = s_kv + wave * 64 * ROW_BYTES, *vl = kl + 32 * ROW_BYTES;
       const uint32_t k_to = lds_address(kl), v_to = lds_address(vl);
       auto rows_of = [&](int i) __attribute__((always_inline)) { return groups(at, (i % PER) * 16 + 4 * wave, std::integral_constant<int, 4>()); };
+      const bool stream = p.stream_rows;
+      auto copy_k = [&](const Groups<4>& g) __attribute__((always_inline)) {
+        if (stream)
+          copy_groups<true, true>(kb, g, pitch, lc, k_to);
+        else
+          copy_groups<true, false>(kb, g, pitch, lc, k_to);
+      };
+      auto copy_v = [&](const Groups<4>& g) __attribute__((always_inline)) {
+        if (stream)
+          copy_groups<false, true>(vb, g, pitch, lc, v_to);
+        else
+          copy_groups<false, false>(vb, g, pitch, lc, v_to);
+      };
       Groups<4> rows = rows_of(0);
-      copy_groups<true>(kb, rows, pitch, lc, k_to);
-      copy_groups<false>(vb, rows, pitch, lc, v_to);
+      copy_k(rows);
+      copy_v(rows);
       for (int i = 0; i < steps; ++i) {
         const int k0 = begin + i * STEP + 32 * wave, k1 = k0 + 31;
         const bool live = k0 <= wave_hi && k1 >= wave_lo, more = i + 1 < steps;
@@ -629,7 +646,7 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) 
             next = ask((i + 1) / PER + 1);
           }
           rows = rows_of(i + 1);
-          copy_groups<true>(kb, rows, pitch, lc, k_to);
+          copy_k(rows);
         }
         u32x4 w[2];
         if (live) {
@@ -648,7 +665,7 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) 
           copies_done();
         if (live) add_values<DT, 1>(vl, w, st);
         lds_read();
-        if (more) copy_groups<false>(vb, rows, pitch, lc, v_to);
+        if (more) copy_v(rows);
       }
     }
   }
