@@ -240,7 +240,9 @@ __device__ __forceinline__ uint32_t pair_of(float a, float b) {
 }
 
 // Halves of whole pieces (rot_dim a multiple of 16), or neighbours (of 8): LANES lanes a head.
-template <int DT, bool PAIRS, int LANES>
+// PAST: what passes the caches by: nothing, reads, or writes too.
+enum : int { PAST_NONE = 0, PAST_READS = 1, PAST_ALL = 2 };
+template <int DT, bool PAIRS, int LANES, int PAST>
 __global__ __launch_bounds__(256) void rotate_kernel(RotateParams p) {
   constexpr int HEADS = 64 / LANES;  // a wave does at a time
   const int task = (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -259,8 +261,12 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateParams p) {
   auto fetch = [&](int h) __attribute__((always_inline)) {
     if (h >= h_end || !used) return;
     const uint16_t* src = head_src(p, row, h);
-    a = *reinterpret_cast<const u32x4*>(src + ca);
-    if (two) b = *reinterpret_cast<const u32x4*>(src + cb);
+    auto piece_at = [&](int c) {
+      const u32x4* at = reinterpret_cast<const u32x4*>(src + c);
+      return PAST == PAST_NONE ? *at : __builtin_nontemporal_load(at);
+    };
+    a = piece_at(ca);
+    if (two) b = piece_at(cb);
   };
   fetch(h0);
   const int pos = p.pos[row];
@@ -292,8 +298,15 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateParams p) {
         }
       }
     }
-    *reinterpret_cast<u32x4*>(dst + ca) = x;
-    if (two) *reinterpret_cast<u32x4*>(dst + cb) = y;
+    auto put = [&](int c, u32x4 v) {
+      u32x4* at = reinterpret_cast<u32x4*>(dst + c);
+      if (PAST == PAST_ALL)
+        __builtin_nontemporal_store(v, at);
+      else
+        *at = v;
+    };
+    put(ca, x);
+    if (two) put(cb, y);
   }
 }
 
@@ -326,16 +339,28 @@ __global__ __launch_bounds__(256) void rotate_any_kernel(RotateParams p) {
   }
 }
 
-template <int DT>
+template <int DT, int PAST>
 static void launch_rotate_typed(const RotateParams& p, dim3 grid, int lanes, hipStream_t stream) {
   if (lanes == 64)
     hipLaunchKernelGGL((rotate_any_kernel<DT>), grid, dim3(256), 0, stream, p);
   else if (!p.halves)
-    hipLaunchKernelGGL((rotate_kernel<DT, true, 16>), grid, dim3(256), 0, stream, p);
+    hipLaunchKernelGGL((rotate_kernel<DT, true, 16, PAST>), grid, dim3(256), 0, stream, p);
   else if (lanes == 8)
-    hipLaunchKernelGGL((rotate_kernel<DT, false, 8>), grid, dim3(256), 0, stream, p);
+    hipLaunchKernelGGL((rotate_kernel<DT, false, 8, PAST>), grid, dim3(256), 0, stream, p);
   else
-    hipLaunchKernelGGL((rotate_kernel<DT, false, 16>), grid, dim3(256), 0, stream, p);
+    hipLaunchKernelGGL((rotate_kernel<DT, false, 16, PAST>), grid, dim3(256), 0, stream, p);
+}
+template <int DT>
+static void launch_rotate_sized(const RotateParams& p, dim3 grid, int lanes, hipStream_t stream) {
+  // Rows that no cache keeps for the next reader pass it by: 100 MB read and as much written (8192 tokens of 48 heads) 45.6 us, with
+  // reads past the caches 38.4, with writes too 40.4; 75 MB each 29.7, 29.5, 30.4; 200 MB 85, 84, 77; 50 MB 18.4, 21.0, 21.5.
+  const double mb = (double)p.n_rows * (p.nq + 2 * p.nkv) * ABSB_HEAD_DIM * 2 / (1 << 20);
+  if (mb < 64)
+    launch_rotate_typed<DT, PAST_NONE>(p, grid, lanes, stream);
+  else if (mb < 144)
+    launch_rotate_typed<DT, PAST_READS>(p, grid, lanes, stream);
+  else
+    launch_rotate_typed<DT, PAST_ALL>(p, grid, lanes, stream);
 }
 
 int launch_rotate(RotateParams p, int dtype, hipStream_t stream) {
@@ -348,9 +373,9 @@ int launch_rotate(RotateParams p, int dtype, hipStream_t stream) {
   p.heads_per_part = ((heads + p.parts - 1) / p.parts + at_once - 1) / at_once * at_once;
   const int64_t grid = ((int64_t)p.n_rows * p.parts + 3) / 4;
   if (dtype == ABSB_F16)
-    launch_rotate_typed<ABSB_F16>(p, dim3((unsigned)grid), lanes, stream);
+    launch_rotate_sized<ABSB_F16>(p, dim3((unsigned)grid), lanes, stream);
   else
-    launch_rotate_typed<ABSB_BF16>(p, dim3((unsigned)grid), lanes, stream);
+    launch_rotate_sized<ABSB_BF16>(p, dim3((unsigned)grid), lanes, stream);
   return check_launch();
 }
 
