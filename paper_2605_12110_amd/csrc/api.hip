@@ -350,11 +350,12 @@ static AttendPhase cut_phase(const PhaseSums& s, int log2_tile, int64_t splits, 
 //   (512 work-groups in all).  Equal ones go in rounds; others leave part of one running behind, hardly any if they start
 //   in falling order, as a causal prompt's do.
 //   32-row tiles are bound by memory, 6.0 TB/s, or, if they are few, by what one work-group can ask for: 0.0093 us a key.
-//   The two share a launch well.  Partial results are written and read once; the merge is a launch of its own.
+//   The two share a launch well.  Partial results are written and read, against the launch's own bytes; the merge is a launch of
+//   its own.
 static double attend_us(const PhaseSums (&s)[2], const AttendPhase (&ph)[2], double pairs, int Hkv) {
-  constexpr double PLACES = 512, KEY_ALONE = 0.018, KEY_PAIRED = 0.036, KEY_NARROW = 0.0093, BYTES_US = 6.0e6, START = 8, MERGE = 5;
+  constexpr double CUS = 256, PLACES = 2 * CUS, KEY_ALONE = 0.018, KEY_PAIRED = 0.036, KEY_NARROW = 0.0093, BYTES_US = 6.0e6, START = 8, MERGE = 5;
   const int parts = ph[0].splits + ph[1].splits;
-  double wide = 0, narrow = 0, bytes = 0, units = 0;
+  double wide = 0, alone = 0, behind_narrow = 0, bytes = 0, units = 0, uneven = 1;
   for (int i = 0; i < 2; ++i) {
     if (!ph[i].owners) continue;
     const bool equal = 20 * s[i].keys >= 19.0 * s[i].tiles * s[i].max_keys;
@@ -367,13 +368,14 @@ static double attend_us(const PhaseSums (&s)[2], const AttendPhase (&ph)[2], dou
       const double behind = n <= PLACES ? 0.0 : ph[i].splits == 1 && 4 * s[i].keys < 3.0 * s[i].tiles * s[i].max_keys ? 0.1 : 0.4;
       wide += equal ? std::ceil(n / PLACES) * longest * key : std::max(longest * key, keys * KEY_PAIRED / PLACES + behind * longest * KEY_PAIRED);
     } else {
-      narrow += (equal ? 0.25 : 0.5) * longest * KEY_NARROW;
-      wide = std::max(wide, longest * KEY_NARROW);
+      alone = std::max(alone, longest * KEY_NARROW);
+      behind_narrow += (equal ? 0.25 : 0.5) * longest * KEY_NARROW;
+      if (equal && n > CUS) uneven = 1 + 0.35 * (std::ceil(n / CUS) * CUS / n - 1);  // compute units with one more than others
     }
   }
-  narrow += bytes / BYTES_US;
-  const double merge = parts > 1 ? MERGE + parts / 16 + 2 * pairs * parts * (ABSB_HEAD_DIM + 2) * 4 / BYTES_US : 0.0;
-  return START + std::max(wide, narrow) + 0.35 * std::min(wide, narrow) + 2 * units / PLACES + merge;
+  const double narrow = std::max(alone, bytes / BYTES_US * uneven + behind_narrow);
+  const double merge = parts > 1 ? MERGE + parts / 16 + (wide > 0 ? 4 : 2) * pairs * parts * (ABSB_HEAD_DIM + 2) * 4 / BYTES_US : 0.0;
+  return START + std::max(wide, narrow) + (alone > 0 ? 0.35 * std::min(wide, narrow) : 0.0) + 2 * units / PLACES + merge;
 }
 
 static int plan_attend(const absb_layer* layer, const absb_batch* batch, const absb_rows* rows, const absb_shared_prefix* shared,
@@ -457,7 +459,8 @@ static int plan_attend(const absb_layer* layer, const absb_batch* batch, const a
       for (int i = 0; i < 2; ++i) ph[i] = cut_phase(s[i], tile[i], (int64_t)std::ceil(whole[i] / stretch - 1e-6), owners[i], slots[i]);
       if (ph[1].splits > most_splits) break;
       const double us = attend_us(s, ph, (double)p.rows * layer->num_q_heads, Hkv);
-      if (cuts > 1 && us >= 0.98 * best) continue;  // (as good as level: fewer parts)
+      // (as good as level: fewer parts, unless they are those of narrow tiles, which are small)
+      if (cuts > 1 && us >= (tile[0] == 7 || tile[1] == 7 ? 0.98 : 0.998) * best) continue;
       best = us;
       p.shared = ph[0];
       p.own = ph[1];
