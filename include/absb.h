@@ -427,8 +427,8 @@ typedef struct absb_page_ring {
  *   row_pos [max_rows] i32, row_slot [max_rows] i64 : of every row, its position in its request and its
  *             slot in the cache, page * P + position % P.  Rows behind the last one get position 0 and
  *             slot -1.
- * All or nothing: if the ring holds too few free pages, or a table row is too short for its request's
- * pages, then no table, no page and no cursor changes, every row_slot is -1 and cursors_out[2] (written
+ * All or nothing: if the ring holds too few free pages, or a table row is too short for the pages that its
+ * request takes or gives back, then no table, no page and no cursor changes, every row_slot is -1 and cursors_out[2] (written
  * with a ring only) says how many pages were missing.  Without a ring, rows beyond the table's width get
  * slot -1.  max_rows is at most 2^30, batch at most 65535; sums of rows and of pages must stay below 2^31.  Reads batch->batch,
  * pt_stride and seq_lens, and layer->page_size. */

@@ -39,13 +39,13 @@ __global__ __launch_bounds__(T) void map_rows_kernel(MapParams p) {
   }
 
   // Prefix sums over the T requests from b0 on, into s_*[0 .. T]; the requests' own values beside them.  Returns how many pages
-  // the tables have no place for.
+  // to take or to give back the tables have no place for.
   auto scan = [&](int b0, bool first) __attribute__((always_inline)) {
     const int b = b0 + tid;
     const int before = b < p.batch ? max(p.before[b], 0) : 0, after = b < p.batch ? max(p.after[b], 0) : 0;
     const int had = (int)(((int64_t)before + P - 1) >> lP), need = (int)(((int64_t)after + P - 1) >> lP);
     const uint32_t v[4] = {(uint32_t)max(after - before, 0), (uint32_t)max(need - had, 0), (uint32_t)max(had - need, 0),
-                           ring ? (uint32_t)max(0, need - max(p.pt_stride, had)) : 0u};
+                           ring ? (uint32_t)max(0, max(need, had) - max(p.pt_stride, min(need, had))) : 0u};
     uint32_t in[4];
     if (!first) __syncthreads();  // what the last chunk left has been read
 #pragma unroll
@@ -140,16 +140,14 @@ __global__ __launch_bounds__(T) void map_rows_kernel(MapParams p) {
     const int g_end = min(give.to, base.give + s_give[T]);
     for (int x0 = max(give.from, base.give) + tid; x0 < g_end; x0 += AT_ONCE * T) {
       int32_t phys[AT_ONCE];
-      bool has[AT_ONCE];
 #pragma unroll
       for (int j = 0; j < AT_ONCE; ++j) {
         const int x = min(x0 + j * T, g_end - 1), i = owner(s_give, x - base.give), page = s_need[i] + (x - base.give - s_give[i]);
-        has[j] = page < p.pt_stride;
-        phys[j] = p.page_table[(int64_t)(b0 + i) * p.pt_stride + min(page, p.pt_stride - 1)];
+        phys[j] = p.page_table[(int64_t)(b0 + i) * p.pt_stride + page];
       }
 #pragma unroll
       for (int j = 0; j < AT_ONCE; ++j)
-        if (x0 + j * T < g_end && has[j]) p.ring[place(tail0, x0 + j * T)] = phys[j];
+        if (x0 + j * T < g_end) p.ring[place(tail0, x0 + j * T)] = phys[j];
     }
     base.rows += s_rows[T];
     base.take += s_take[T];
@@ -163,7 +161,7 @@ __global__ __launch_bounds__(T) void map_rows_kernel(MapParams p) {
   }
   if (!ring) return;
   // The cursors: by the work-group that comes last, since all the others have read them by then.
-  if (nwg > 1) __syncthreads();
+  __syncthreads();
   if (tid == 0) {
     unsigned long long* done = reinterpret_cast<unsigned long long*>(p.cursors_out + 3);
     if (nwg == 1 || __hip_atomic_fetch_add(done, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned long long)nwg - 1) {

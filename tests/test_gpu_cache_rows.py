@@ -160,6 +160,23 @@ def test_map_rows_when_many_pages_come_back():
     _map_case([900] * 2000 + [3], [0] * 2000 + [9], 8, in_place=False)
 
 
+@pytest.mark.parametrize("before,after,width,missing", [([90, 5], [0, 6], 2, 10), ([90, 5], [20, 30], 2, 11), ([40], [0], 0, 5)])
+def test_map_rows_of_tables_too_narrow_for_what_comes_back(before, after, width, missing):
+    """Pages of 8: a request shrinks that would hold more of them than its table has entries for.  Nothing changes."""
+    torch, absb = _torch(), _absb()
+    B = len(before)
+    table = torch.arange(B * width, dtype=torch.int32, device="cuda").view(B, width)
+    pages, cursors = torch.arange(100, 120, dtype=torch.int32, device="cuda"), torch.tensor([0, 8, 0, 0], dtype=torch.int64, device="cuda")
+    off, pos = torch.zeros(B + 1, dtype=torch.int32, device="cuda"), torch.zeros(40, dtype=torch.int32, device="cuda")
+    slot = torch.zeros(40, dtype=torch.int64, device="cuda")
+    up = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")  # noqa: E731
+    batch = absb.Batch(seq_lens_host=after, seq_lens=up(after), page_table=table, pt_stride=width)
+    absb.absb_map_rows(_layer(P=8), batch, up(before), table, off, pos, slot, absb.PageRing(pages, cursors))
+    torch.cuda.synchronize()
+    assert cursors.tolist() == [0, 8, missing, 0] and (slot == -1).all()
+    assert table.flatten().tolist() == list(range(B * width)) and pages.tolist() == list(range(100, 120))
+
+
 def test_map_rows_pads_and_cuts_at_max_rows():
     _map_case([3, 0], [9, 30], 8, max_rows=50)
     _map_case([3, 0], [9, 30], 8, max_rows=10)
