@@ -394,7 +394,7 @@ ABSB_API int absb_assign_block_sizes(int32_t n_samples, int32_t n_heads, int32_t
  * everything their requests hold, on the same paged caches and page tables as the rest of the library.
  * They read layer->num_q_heads, num_kv_heads, head_dim, page_size, dtype, the K/V strides (kv_stride_tok
  * at most 2^28) and sm_scale; block sizes and the selection policy do not matter to them
- * (layer->block_size may be NULL).  Lengths may be 0 here, and at most 2^30; rows times query heads stay below 2^31.
+ * (layer->block_size may be NULL).  Lengths may be 0 here, and at most 2^30; rows times query heads stay below 2^30.
  *
  * "Rows": the new tokens of all requests side by side, request b's at [row_off[b], row_off[b+1]).  They
  * are the LAST tokens of their context: with n_b rows and length L_b (which counts them), row
@@ -468,6 +468,7 @@ typedef struct absb_rope {
 ABSB_API int absb_rope_frequencies(const absb_rope* rope, double* freq_host);
 
 /* Rotates queries and keys to their positions and writes keys and values into the paged caches.
+ *   n_rows    : below 2^26
  *   row_pos [n_rows] i32, row_slot [n_rows] i64 : as absb_map_rows writes them.  A row whose slot is negative
  *             has its query rotated and nothing stored.  Two rows with one slot: either is kept.
  *   freq [rot_dim/2] f64 device : radians per position, |freq| < 2^32.  Angles are exact to 2^-32 turns + position *
@@ -517,7 +518,9 @@ ABSB_API int absb_attend_workspace(const absb_layer* layer, const absb_batch* ba
  * mixture.
  *   q, out [rows][Hq][d] (16-byte aligned; out may be q), lse [rows][Hq] f32 optional (NULL ok)
  *   opts : NULL = causal attention and nothing else
- * Reads batch->batch, seq_lens(_host), page_table and pt_stride (>= ceil(max L_b / P)).  Slots beyond a
+ * Reads batch->batch, seq_lens(_host), page_table and pt_stride (>= ceil(max L_b / P)).  The host's lengths only bound the
+ * work that is enqueued: a captured call follows the lengths that it finds on the device, as long as none exceeds its
+ * host twin, row_off (and groups) are the same, and each is at least its rows (and its group's shared tokens beside them).  Slots beyond a
  * context may hold anything; the tokens of a context must be finite, also those that the row does not see.
  * Accumulation, maxima and sums are binary32; the softmax weights enter the product with V rounded to the K/V
  * type, their sum is taken before rounding. */

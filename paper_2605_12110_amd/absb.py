@@ -574,6 +574,8 @@ def absb_rotate_store(layer: Layer, rope: Rope, row_pos, row_slot, freq, q=None,
     qs = 0 if q is None else _row_stride(q, n, cl.num_q_heads, where)
     ks = 0 if k is None else _row_stride(k, n, cl.num_kv_heads, where)
     vs = 0 if v is None else _row_stride(v, n, cl.num_kv_heads, where)
+    if row_slot is not None and row_slot.numel() != n:
+        raise AbsbError(ERR_BAD_SHAPE, where)
     if q_out is not None and (not q_out.is_contiguous() or q_out.numel() != n * cl.num_q_heads * 128):
         raise AbsbError(ERR_BAD_SHAPE, where)
     _check(load().absb_rotate_store(C.byref(cl), _rec(rope), n, _ptr(row_pos), _ptr(row_slot), _ptr(freq), _ptr(q), qs, _ptr(q_out),
@@ -588,16 +590,18 @@ def absb_attend_workspace(layer: Layer, batch: Batch, rows: Rows, shared: Shared
     return int(n.value)
 
 
-def _dense(where: str, *tensors) -> None:
+def _dense(where: str, heads: int, rows: Rows, *tensors) -> None:
+    """Queries and outputs: dense, and as many rows as the step has."""
     for t in tensors:
-        if t is not None and t.__class__ is not int and not t.is_contiguous():
-            raise AbsbError(ERR_BAD_SHAPE, where)
+        if t is not None and t.__class__ is not int:
+            if not t.is_contiguous() or (rows.row_off_host is not None and t.numel() < int(rows.row_off_host[-1]) * heads * 128):
+                raise AbsbError(ERR_BAD_SHAPE, where)
 
 
 def absb_attend_rows(layer: Layer, batch: Batch, rows: Rows, q, k_cache, v_cache, out, lse=None, opts: ScoreOpts = None,
                      workspace=None, stream=None) -> None:
     cl, cb = layer.c(), batch.c()
-    _dense("absb_attend_rows", q, out)
+    _dense("absb_attend_rows", cl.num_q_heads, rows, q, out)
     _check(load().absb_attend_rows(C.byref(cl), C.byref(cb), _rec(rows), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(out), _ptr(lse),
                                    _rec(opts), _ptr(workspace), _nbytes(workspace), _stream(stream)), "absb_attend_rows")
 
@@ -605,7 +609,7 @@ def absb_attend_rows(layer: Layer, batch: Batch, rows: Rows, q, k_cache, v_cache
 def absb_attend_shared(layer: Layer, batch: Batch, rows: Rows, shared: SharedPrefix, q, k_cache, v_cache, out, lse=None,
                        opts: ScoreOpts = None, workspace=None, stream=None) -> None:
     cl, cb = layer.c(), batch.c()
-    _dense("absb_attend_shared", q, out)
+    _dense("absb_attend_shared", cl.num_q_heads, rows, q, out)
     _check(load().absb_attend_shared(C.byref(cl), C.byref(cb), _rec(rows), _rec(shared), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(out),
                                      _ptr(lse), _rec(opts), _ptr(workspace), _nbytes(workspace), _stream(stream)), "absb_attend_shared")
 

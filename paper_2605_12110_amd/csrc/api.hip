@@ -395,7 +395,7 @@ static int plan_attend(const absb_layer* layer, const absb_batch* batch, const a
     max_n = std::max<int64_t>(max_n, off[b + 1] - off[b]);
   }
   if ((int64_t)batch->pt_stride < ceil_div(max_len, P)) return ABSB_ERR_BAD_SHAPE;
-  if ((int64_t)off[Bt] * layer->num_q_heads >= int64_t(1) << 31) return ABSB_ERR_BAD_SHAPE;  // (queries of half a terabyte)
+  if ((int64_t)off[Bt] * layer->num_q_heads >= int64_t(1) << 30) return ABSB_ERR_BAD_SHAPE;  // (queries of 256 GiB)
   AttendPlan p = {};
   p.rows = off[Bt];
   PhaseSums sums[2];  // shared keys, own keys
@@ -450,6 +450,7 @@ static int plan_attend(const absb_layer* layer, const absb_batch* batch, const a
   // Both phases' keys are cut into stretches that take about equally long (a narrow tile's key takes half of a wide one's).
   const int64_t owners[2] = {shared ? shared->groups : 0, Bt};
   const int64_t slots[2] = {(((int64_t)off[Bt] * G) >> tile[0]) + owners[0], (((int64_t)off[Bt] * G) >> tile[1]) + Bt};
+  auto work_groups = [&](const AttendPhase (&ph)[2]) { return (ph[0].slots * ph[0].splits + ph[1].slots * ph[1].splits) * Hkv; };
   auto choose = [&](const PhaseSums (&s)[2], int most_splits) {
     double whole[2], best = 0;
     for (int i = 0; i < 2; ++i) whole[i] = s[i].max_keys * (tile[i] == 7 ? 2.0 : 1.0);
@@ -457,7 +458,7 @@ static int plan_attend(const absb_layer* layer, const absb_batch* batch, const a
       AttendPhase ph[2];
       const double stretch = std::max(whole[0], whole[1]) / cuts;
       for (int i = 0; i < 2; ++i) ph[i] = cut_phase(s[i], tile[i], (int64_t)std::ceil(whole[i] / stretch - 1e-6), owners[i], slots[i]);
-      if (ph[1].splits > most_splits) break;
+      if (ph[1].splits > most_splits || (cuts > 1 && work_groups(ph) > MAX_WGS)) break;
       const double us = attend_us(s, ph, (double)p.rows * layer->num_q_heads, Hkv);
       // (as good as level: fewer parts, unless they are those of narrow tiles, which are small)
       if (cuts > 1 && us >= (tile[0] == 7 || tile[1] == 7 ? 0.98 : 0.998) * best) continue;
@@ -482,7 +483,7 @@ static int plan_attend(const absb_layer* layer, const absb_batch* batch, const a
   }
   p.parts = p.shared.splits + p.own.splits;
   const int ws_parts = any_options ? parts_any : p.parts;
-  if (p.shared.slots * Hkv * p.shared.splits + p.own.slots * Hkv * p.own.splits >= (int64_t(1) << 31)) return ABSB_ERR_BAD_SHAPE;
+  if (work_groups({p.shared, p.own}) > MAX_WGS) return ABSB_ERR_BAD_SHAPE;
   // Narrow tiles read a row once; what the last-level cache could not keep for the next call anyway passes it by (one token behind
   // 128 K 101 -> 88 us, 64 behind 2 K 95 -> 84, 64 behind 1 K, 134 MB, 50.3 -> 44.7).
   p.stream_rows = (sums[0].owners_keys + sums[1].owners_keys) * Hkv * 4 * ABSB_HEAD_DIM >= 96.0 * (1 << 20);
@@ -821,7 +822,7 @@ int absb_rotate_store(const absb_layer* layer, const absb_rope* rope, int32_t n_
   if (rc != ABSB_OK) return rc;
   rc = check_rope(rope);
   if (rc != ABSB_OK) return rc;
-  if (n_rows < 0) return ABSB_ERR_BAD_SHAPE;
+  if (n_rows < 0 || n_rows >= 1 << 26) return ABSB_ERR_BAD_SHAPE;  // (four rows a work-group)
   if (n_rows == 0) return ABSB_OK;
   if (!row_pos || !freq || !q != !q_out || !k != !v || (!q && !k)) return ABSB_ERR_NULL;
   if (k && (!row_slot || !k_cache || !v_cache)) return ABSB_ERR_NULL;
@@ -891,7 +892,6 @@ static int attend(const absb_layer* layer, const absb_batch* batch, const absb_r
   p.page_table = batch->page_table;
   p.seq_lens = batch->seq_lens;
   p.row_off = rows->row_off;
-  p.batch = batch->batch;
   if (plan.shared.owners) {
     p.first = shared->first;
     p.len = shared->len;

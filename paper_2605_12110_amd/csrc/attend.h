@@ -4,6 +4,9 @@
 
 namespace absb {
 
+// Work-groups of 256 threads that a launch can have: its threads are counted in 32 bits.
+constexpr int64_t MAX_WGS = (int64_t(1) << 24) - 1;
+
 // A phase of a call: the rows of "owners" against the keys that an owner holds.  Own keys: an owner is a request.  Shared keys: an
 // owner is a group of requests, its keys the group's prefix.  An owner's rows, n tokens of G query heads a KV head, are cut
 // into tiles; owner o's tiles are slots floor(row_off[o] * G / tile) + o and on, which leaves room for all of them
@@ -36,7 +39,7 @@ struct AttendParams {
   float* part_o;   // [rows][Hq][parts][128], not normalised
   float* part_ml;  // [rows][Hq][parts][2]: maximum in log2 units, sum
   int64_t s_page, s_head, s_tok;  // bytes
-  int32_t batch, groups, pt_stride, Hq, Hkv, G, log2_page;
+  int32_t groups, pt_stride, Hq, Hkv, G, log2_page;
   int32_t inv_G;                  // 2^16 / G, rounded up
   int32_t window, parts;
   int32_t stream_rows;            // 1: narrow tiles read rows past the caches

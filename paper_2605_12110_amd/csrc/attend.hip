@@ -13,6 +13,7 @@
 // K and V are copied from their pages straight to LDS, a block ahead, 16 bytes a lane.  The copy writes lanes side by side, so
 // what spreads a read over the banks is which piece of a row a lane fetches: K's piece p of row r lies at p ^ (r % 16), V's at
 // p ^ 4 (r % 4).
+#include <algorithm>
 #include <type_traits>
 
 #include "attend.h"
@@ -744,45 +745,45 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) 
 // The parts of a (row, query head), a wave each: half a wave a part, a lane four channels.
 template <int DT>
 __global__ __launch_bounds__(256) void attend_merge_kernel(AttendParams p, int64_t pairs) {
-  const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (at >= pairs) return;
   const int lane = threadIdx.x & 63, half = lane >> 5;
-  const float* ml = p.part_ml + at * p.parts * 2;
-  const float* o = p.part_o + at * p.parts * ABSB_HEAD_DIM + 4 * (lane & 31);
-  constexpr int TRIP = 16;  // parts fetched at once
-  float M = -__builtin_inff(), L = 0.0f;
-  f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int i0 = 0; i0 < p.parts; i0 += 64) {
-    float2 mine = make_float2(-__builtin_inff(), 0.0f);
-    if (i0 + lane < p.parts) mine = *reinterpret_cast<const float2*>(ml + (i0 + lane) * 2);
-    if (mine.y == 0.0f) mine.x = -__builtin_inff();  // (a NaN stays one)
-    const float top = fmaxf(M, wave_max_f32(mine.x)), base = top == -__builtin_inff() ? 0.0f : top;
-    const float a = exp2_fast(M - base), w = exp2_fast(mine.x - base);
-    M = top;
-    L = __builtin_fmaf(L, a, mine.y * w);  // (a lane's own parts)
-    x *= a;
-    const int n = min(64, p.parts - i0);
-    for (int i = 0; i < n; i += TRIP) {
-      f32x4 v[TRIP / 2];
+  for (int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); at < pairs; at += (int64_t)gridDim.x * 4) {
+    const float* ml = p.part_ml + at * p.parts * 2;
+    const float* o = p.part_o + at * p.parts * ABSB_HEAD_DIM + 4 * (lane & 31);
+    constexpr int TRIP = 16;  // parts fetched at once
+    float M = -__builtin_inff(), L = 0.0f;
+    f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int i0 = 0; i0 < p.parts; i0 += 64) {
+      float2 mine = make_float2(-__builtin_inff(), 0.0f);
+      if (i0 + lane < p.parts) mine = *reinterpret_cast<const float2*>(ml + (i0 + lane) * 2);
+      if (mine.y == 0.0f) mine.x = -__builtin_inff();  // (a NaN stays one)
+      const float top = fmaxf(M, wave_max_f32(mine.x)), base = top == -__builtin_inff() ? 0.0f : top;
+      const float a = exp2_fast(M - base), w = exp2_fast(mine.x - base);
+      M = top;
+      L = __builtin_fmaf(L, a, mine.y * w);  // (a lane's own parts)
+      x *= a;
+      const int n = min(64, p.parts - i0);
+      for (int i = 0; i < n; i += TRIP) {
+        f32x4 v[TRIP / 2];
 #pragma unroll
-      for (int j = 0; j < TRIP / 2; ++j)
-        v[j] = *reinterpret_cast<const f32x4*>(o + (int64_t)(i0 + min(i + 2 * j + half, n - 1)) * ABSB_HEAD_DIM);
+        for (int j = 0; j < TRIP / 2; ++j)
+          v[j] = *reinterpret_cast<const f32x4*>(o + (int64_t)(i0 + min(i + 2 * j + half, n - 1)) * ABSB_HEAD_DIM);
 #pragma unroll
-      for (int j = 0; j < TRIP / 2; ++j) {
-        const float wi = __shfl(w, min(i + 2 * j + half, 63));
-        if (i + 2 * j + half < n && wi != 0.0f) x += v[j] * wi;  // (an output of weight 0 may never have been written)
+        for (int j = 0; j < TRIP / 2; ++j) {
+          const float wi = __shfl(w, min(i + 2 * j + half, 63));
+          if (i + 2 * j + half < n && wi != 0.0f) x += v[j] * wi;  // (an output of weight 0 may never have been written)
+        }
       }
     }
-  }
 #pragma unroll
-  for (int j = 0; j < 4; ++j) x[j] = across_halves(x[j], [](float a, float b) { return a + b; });
-  L = row16_sum(L);
-  L = bitcast<float>(__builtin_amdgcn_readlane(bitcast<int>(L), 0)) + bitcast<float>(__builtin_amdgcn_readlane(bitcast<int>(L), 16)) +
-      bitcast<float>(__builtin_amdgcn_readlane(bitcast<int>(L), 32)) + bitcast<float>(__builtin_amdgcn_readlane(bitcast<int>(L), 48));
-  const float inv = L == 0.0f ? 0.0f : 1.0f / L;
-  if (half == 0)
-    *reinterpret_cast<uint2*>(p.out + at * ABSB_HEAD_DIM + 4 * lane) = uint2{pack2<DT>(x[0] * inv, x[1] * inv), pack2<DT>(x[2] * inv, x[3] * inv)};
-  if (p.lse && lane == 0) p.lse[at] = L == 0.0f ? -__builtin_inff() : (M + __builtin_log2f(L)) * LN2;
+    for (int j = 0; j < 4; ++j) x[j] = across_halves(x[j], [](float a, float b) { return a + b; });
+    L = row16_sum(L);
+    L = bitcast<float>(__builtin_amdgcn_readlane(bitcast<int>(L), 0)) + bitcast<float>(__builtin_amdgcn_readlane(bitcast<int>(L), 16)) +
+        bitcast<float>(__builtin_amdgcn_readlane(bitcast<int>(L), 32)) + bitcast<float>(__builtin_amdgcn_readlane(bitcast<int>(L), 48));
+    const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+    if (half == 0)
+      *reinterpret_cast<uint2*>(p.out + at * ABSB_HEAD_DIM + 4 * lane) = uint2{pack2<DT>(x[0] * inv, x[1] * inv), pack2<DT>(x[2] * inv, x[3] * inv)};
+    if (p.lse && lane == 0) p.lse[at] = L == 0.0f ? -__builtin_inff() : (M + __builtin_log2f(L)) * LN2;
+  }
 }
 
 template <int DT, int CAP, bool BIAS>
@@ -791,7 +792,8 @@ static void launch_parts(const AttendParams& p, int64_t rows, hipStream_t stream
   hipLaunchKernelGGL((attend_kernel<DT, CAP, BIAS>), dim3((unsigned)(p.shared_units + own_units)), dim3(ATT_THREADS), 0, stream, p);
   if (p.parts > 1) {
     const int64_t pairs = rows * p.Hq;
-    hipLaunchKernelGGL((attend_merge_kernel<DT>), dim3((unsigned)((pairs + 3) / 4)), dim3(256), 0, stream, p, pairs);
+    const unsigned grid = (unsigned)std::min<int64_t>((pairs + 3) / 4, MAX_WGS);
+    hipLaunchKernelGGL((attend_merge_kernel<DT>), dim3(grid), dim3(256), 0, stream, p, pairs);
   }
 }
 template <int DT, int CAP>

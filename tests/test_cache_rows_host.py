@@ -211,6 +211,21 @@ def test_attend_refuses_null_records():
     assert lib.absb_attend_shared(C.byref(cl), C.byref(cb), C.byref(cr), None, AT, AT, AT, AT, None, None, None, 0, None) == absb.ERR_NULL
 
 
+def test_what_a_launch_or_a_tensor_cannot_hold_is_refused():
+    _refused(absb.ERR_BAD_SHAPE, absb.absb_rotate_store, **_rot(n=1 << 26))
+    _refused(absb.ERR_BAD_SHAPE, absb.absb_rotate_store, **_rot(row_slot=_T(2)))
+    _refused(absb.ERR_BAD_SHAPE, absb.absb_attend_rows, *_att(lens=(1 << 25, 1), new=(1 << 25, 0), ws=BIG_WS))   # 2^30 pairs of row and head
+    for kw in (dict(q=_T(2, 32, D)), dict(out=_T(3, 31, D))):
+        _refused(absb.ERR_BAD_SHAPE, absb.absb_attend_rows, *_att(**kw))
+    # many requests of which one is long: cut no further than a launch has room for, and refused if it never had
+    n, layer = 65535, _layer(num_q_heads=64, num_kv_heads=64)
+    lens = np.full(n, 64, np.int32)
+    lens[0] = 1 << 30
+    batch, rows = absb.Batch(seq_lens_host=lens, seq_lens=AT, page_table=AT, pt_stride=1 << 24), _rows(np.ones(n, np.int32))
+    parts = absb.absb_attend_workspace(layer, batch, rows, None, absb.ScoreOpts()) // (n * 64 * 520)
+    assert parts <= 3             # 65535 + 65535 / 32 slots of 64 heads are a quarter of the work-groups of a launch
+
+
 def test_attend_of_no_rows_does_nothing():
     absb.absb_attend_rows(*_att(new=(0, 0)), stream=0)
     absb.absb_attend_rows(*_att(lens=(0, 0), new=(0, 0), q=None, out=None), stream=0)

@@ -659,6 +659,28 @@ def test_attend_is_the_same_every_time_and_in_a_graph():
             assert torch.equal(c.out[:c.rows], want[:c.rows]) and torch.equal(c.lse[:c.rows], want_lse[:c.rows])
 
 
+@pytest.mark.parametrize("kw", [dict(lens=[9000, 700, 40, 3], new=[1, 1, 1, 1]), dict(lens=[3000, 2500], new=[70, 200]),
+                                dict(lens=[6000, 6000, 5900, 2300], new=[1, 1, 1, 2], shared=[2048], P=32),
+                                dict(lens=[6000, 6000], new=[1, 40], window=300)])
+def test_a_captured_call_follows_the_lengths_it_finds(kw):
+    """Planned for the longest, replayed at shorter ones: a row's context is what the device's lengths say."""
+    torch = _torch()
+    c = Call(**kw)
+    c.run()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        c.run()
+    least = np.asarray(kw["new"]) + (kw["shared"][0] if "shared" in kw else 0)
+    for step, part in enumerate((0.0, 0.3, 0.8, 1.0)):
+        c.lens = (least + (np.asarray(kw["lens"]) - least) * part).astype(np.int32)
+        c.batch.seq_lens.copy_(torch.from_numpy(c.lens))
+        c.ws.fill_(0x7f)
+        c.run = g.replay
+        c.check(f"lengths {c.lens.tolist()}")
+
+
 @pytest.mark.parametrize("lens,new", [([9000], [1]), ([2100, 17, 900], [1, 1, 1]), ([6000] + [100] * 20, [1] * 21), ([3000, 2000], [40, 3])])
 def test_attend_workspace_holds_for_every_window(lens, new):
     torch = _torch()
