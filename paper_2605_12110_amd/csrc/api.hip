@@ -388,7 +388,7 @@ static int plan_attend(const absb_layer* layer, const absb_batch* batch, const a
   if (Bt < 1 || Bt > 65535) return ABSB_ERR_BAD_SHAPE;
   const int32_t *off = rows->row_off_host, *lens = batch->seq_lens_host;
   if (off[0] != 0) return ABSB_ERR_BAD_SHAPE;
-  int64_t max_len = 0, max_n = 0;
+  int64_t max_len = 0, max_n = 0, most = 0;  // ... rows of a group
   for (int b = 0; b < Bt; ++b) {
     if (off[b + 1] < off[b] || off[b + 1] - off[b] > lens[b] || lens[b] > (1 << 30)) return ABSB_ERR_BAD_SHAPE;
     max_len = std::max<int64_t>(max_len, lens[b]);
@@ -404,7 +404,6 @@ static int plan_attend(const absb_layer* layer, const absb_batch* batch, const a
   if (shared) {
     const int32_t* first = shared->first_host;
     if (shared->groups < 1 || first[0] != 0) return ABSB_ERR_BAD_SHAPE;
-    int64_t most = 0;
     for (int g = 0; g < shared->groups; ++g) {
       if (first[g + 1] < first[g] || first[g + 1] > Bt) return ABSB_ERR_BAD_SHAPE;
       const int32_t len = shared->len_host[g];
@@ -484,9 +483,13 @@ static int plan_attend(const absb_layer* layer, const absb_batch* batch, const a
   p.parts = p.shared.splits + p.own.splits;
   const int ws_parts = any_options ? parts_any : p.parts;
   if (work_groups({p.shared, p.own}) > MAX_WGS) return ABSB_ERR_BAD_SHAPE;
-  // Narrow tiles read a row once; what the last-level cache could not keep for the next call anyway passes it by (one token behind
-  // 128 K 101 -> 88 us, 64 behind 2 K 95 -> 84, 64 behind 1 K, 134 MB, 50.3 -> 44.7).
-  p.stream_rows = (sums[0].owners_keys + sums[1].owners_keys) * Hkv * 4 * ABSB_HEAD_DIM >= 96.0 * (1 << 20);
+  // Owners of one tile have their rows read once; what the last-level cache could not keep for the next call anyway passes it by.
+  // Narrow: one token behind 128 K 101 -> 88 us, 64 behind 2 K 95 -> 84, 64 behind 1 K, 134 MB, 50.3 -> 44.7.  Wide: 12 behind 128 K
+  // 110 -> 97 us, 64 times 12 behind 2 K 134 -> 122, but 32 tokens behind 32 K shared ones, 134 MB, 41.6 -> 43.3.
+  const double mib = (sums[0].owners_keys + sums[1].owners_keys) * Hkv * 4 * ABSB_HEAD_DIM / (1 << 20);
+  auto past = [&](int log2_tile, int64_t most_rows) { return most_rows * G <= int64_t(1) << log2_tile && mib >= (log2_tile == 7 ? 192 : 96); };
+  p.shared.stream = past(tile[0], most);
+  p.own.stream = past(tile[1], max_n);
   const int64_t pairs = p.rows * layer->num_q_heads;
   if (ws_parts > 1) {
     p.ws_part_ml = align256((size_t)pairs * ws_parts * ABSB_HEAD_DIM * 4);
@@ -917,7 +920,6 @@ static int attend(const absb_layer* layer, const absb_batch* batch, const absb_r
   p.inv_G = (65536 + p.G - 1) / p.G;
   p.log2_page = ilog2(layer->page_size);
   p.parts = plan.parts;
-  p.stream_rows = plan.stream_rows;
   p.shared = plan.shared;
   p.own = plan.own;
   p.shared_units = (uint32_t)(plan.shared.slots * p.Hkv * plan.shared.splits);

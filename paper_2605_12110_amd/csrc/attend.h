@@ -16,6 +16,7 @@ struct AttendPhase {
   int32_t log2_tile;  // rows (token, query head of the group) of a work-group: 128, or 32 that its four waves share
   int32_t splits;  // of a tile's keys, a work-group each
   int32_t chunk;   // keys of a split, a multiple of 128
+  int32_t stream;  // 1: rows are read past the caches
   int64_t slots;   // tiles, empty ones included
 };
 
@@ -23,7 +24,6 @@ struct AttendPlan {
   AttendPhase shared, own;  // shared.owners = 0: no such phase
   int32_t parts;            // partial results of a row: shared.splits + own.splits
   int64_t rows;
-  int32_t stream_rows;
   size_t ws_part_ml, ws_bytes;  // ws_bytes = 0: one part, written straight to the output
 };
 
@@ -42,7 +42,6 @@ struct AttendParams {
   int32_t groups, pt_stride, Hq, Hkv, G, log2_page;
   int32_t inv_G;                  // 2^16 / G, rounded up
   int32_t window, parts;
-  int32_t stream_rows;            // 1: narrow tiles read rows past the caches
   float scale_log2;               // sm_scale * log2(e)
   float cap_log2, cap_in;         // cap * log2(e), 2 log2(e) sm_scale / cap (capped only)
   uint32_t shared_units;          // work-groups of the first phase, ahead of the second's

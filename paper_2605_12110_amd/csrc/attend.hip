@@ -470,6 +470,7 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) 
   const uint32_t unit = shared ? blockIdx.x : blockIdx.x - p.shared_units;
   const AttendPhase& ph = shared ? p.shared : p.own;
   const int owners = ph.owners, splits = ph.splits, log2_tile = ph.log2_tile, chunk = ph.chunk;
+  const bool stream = ph.stream;
   const int part0 = shared ? 0 : p.shared.splits;
   const bool wide = log2_tile == 7;
   const int kv_head = (int)(unit % (uint32_t)p.Hkv);
@@ -558,13 +559,14 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) 
     };
     Stretch at = stretch(0, ask(0));
     int32_t next = ask(1);
-    if (wide) {
+    auto wide_tile = [&](auto past) __attribute__((always_inline)) {
+      constexpr bool STREAM = decltype(past)::value;
       constexpr int STEP = 64, PER = 512 / STEP, STAGE = STEP * ROW_BYTES;
       const int steps = (end - begin + STEP - 1) / STEP;
       const char* mine = s_kv;
       const uint32_t to = lds_address(s_kv) + 16 * wave * ROW_BYTES;
-      auto copy_k = [&](const Groups<2>& g, int i) __attribute__((always_inline)) { copy_groups<true, false>(kb, g, pitch, lc, to + (i & 1) * STAGE); };
-      auto copy_v = [&](const Groups<2>& g, int i) __attribute__((always_inline)) { copy_groups<false, false>(vb, g, pitch, lc, to + (2 + (i & 1)) * STAGE); };
+      auto copy_k = [&](const Groups<2>& g, int i) __attribute__((always_inline)) { copy_groups<true, STREAM>(kb, g, pitch, lc, to + (i & 1) * STAGE); };
+      auto copy_v = [&](const Groups<2>& g, int i) __attribute__((always_inline)) { copy_groups<false, STREAM>(vb, g, pitch, lc, to + (2 + (i & 1)) * STAGE); };
       auto rows_of = [&](int i) __attribute__((always_inline)) { return groups(at, (i % PER) * 8 + 2 * wave, std::integral_constant<int, 2>()); };
       Groups<2> rows = rows_of(0);
       // Step i: the scores of block i + 1 are worked out beside the softmax of block i, matrix and vector unit at once; so K is
@@ -610,6 +612,12 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) 
         step(i, s0, s1);
         if (i + 1 < steps) step(i + 1, s1, s0);
       }
+    };
+    if (wide) {
+      if (stream)
+        wide_tile(std::true_type());
+      else
+        wide_tile(std::false_type());
     } else {
       // Every wave by itself, 32 keys a step: K's buffer takes the next block's as soon as the scores have been worked out, V's as
       // soon as the output has, so that copies are in flight all the time and no two waves wait for each other.
@@ -618,7 +626,6 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) 
       const char *kl = s_kv + wave * 64 * ROW_BYTES, *vl = kl + 32 * ROW_BYTES;
       const uint32_t k_to = lds_address(kl), v_to = lds_address(vl);
       auto rows_of = [&](int i) __attribute__((always_inline)) { return groups(at, (i % PER) * 16 + 4 * wave, std::integral_constant<int, 4>()); };
-      const bool stream = p.stream_rows;
       auto copy_k = [&](const Groups<4>& g) __attribute__((always_inline)) {
         if (stream)
           copy_groups<true, true>(kb, g, pitch, lc, k_to);

@@ -539,6 +539,12 @@ def test_attend_windows_over_splits_of_odd_groups(Hq, Hkv):
         Call([9001, 333], [1, 2], Hq, Hkv, 16, "f16", window=window).check(f"tokens, window {window}, {Hq} heads")
 
 
+@pytest.mark.parametrize("lens,new,shared", [([50011], [1], None), ([50011], [12], None), ([25000, 26003], [17, 3], None), ([51000, 50500], [5, 4], [50176])])
+def test_attend_past_the_caches(lens, new, shared):
+    """Contexts of 200 MB, narrow tiles and wide ones, own and shared."""
+    Call(lens, new, 32, 8, 64, shared=shared, seed=5).check(f"{lens} {new} {shared}")
+
+
 def test_attend_of_more_than_64_parts():
     absb = _absb()
     c = Call([120001], [1], 8, 1, 64, "f16", shared=[60032])
