@@ -352,8 +352,15 @@ static AttendPhase cut_phase(const PhaseSums& s, int log2_tile, int64_t splits, 
 //   32-row tiles are bound by memory, 6.0 TB/s, or, if they are few, by what one work-group can ask for: 0.0093 us a key.
 //   The two share a launch well.  Partial results are written and read, against the launch's own bytes; the merge is a launch of
 //   its own.
-static double attend_us(const PhaseSums (&s)[2], const AttendPhase (&ph)[2], double pairs, int Hkv) {
+// `whole`: tiles of the second phase that are not cut (then they are equal, and the only phase's).
+static double attend_us(const PhaseSums (&s)[2], const AttendPhase (&ph)[2], double pairs, int Hkv, int64_t whole) {
   constexpr double CUS = 256, PLACES = 2 * CUS, KEY_ALONE = 0.018, KEY_PAIRED = 0.036, KEY_NARROW = 0.0093, BYTES_US = 6.0e6, START = 8, MERGE = 5;
+  auto key_us = [&](double n) { return KEY_ALONE + (KEY_PAIRED - KEY_ALONE) * std::min(1.0, n / PLACES); };
+  auto rounds = [&](double n) {  // us a key; behind a full round compute units get a second work-group only when all have one
+    const double full = std::floor(n / PLACES), rest = n - full * PLACES;
+    if (full == 0) return key_us(n);
+    return full * KEY_PAIRED + (rest > 0 ? KEY_ALONE + (KEY_PAIRED - KEY_ALONE) * std::max(0.0, rest / CUS - 1) : 0.0);
+  };
   const int parts = ph[0].splits + ph[1].splits;
   double wide = 0, alone = 0, behind_narrow = 0, bytes = 0, units = 0, uneven = 1;
   for (int i = 0; i < 2; ++i) {
@@ -362,11 +369,17 @@ static double attend_us(const PhaseSums (&s)[2], const AttendPhase (&ph)[2], dou
     const double tiles = (double)s[i].tiles * Hkv, keys = s[i].keys * Hkv, longest = (double)std::min<int64_t>(ph[i].chunk, s[i].max_keys);
     const double n = ph[i].splits == 1 ? tiles : equal ? tiles * ph[i].splits : std::max(tiles, keys / ph[i].chunk + 0.5 * tiles);
     bytes += s[i].owners_keys * Hkv * 4 * ABSB_HEAD_DIM;
+    if (whole) {
+      const double rest = (tiles - whole * Hkv) * ph[i].splits;
+      wide = rounds(whole * Hkv) * s[i].max_keys + rounds(rest) * longest;
+      units = whole * Hkv + rest;
+      pairs *= 1.0 - whole * Hkv / tiles;
+      continue;
+    }
     units += n;
     if (ph[i].log2_tile == 7) {
-      const double key = KEY_ALONE + (KEY_PAIRED - KEY_ALONE) * std::min(1.0, n / PLACES);
       const double behind = n <= PLACES ? 0.0 : ph[i].splits == 1 && 4 * s[i].keys < 3.0 * s[i].tiles * s[i].max_keys ? 0.1 : 0.4;
-      wide += equal ? std::ceil(n / PLACES) * longest * key : std::max(longest * key, keys * KEY_PAIRED / PLACES + behind * longest * KEY_PAIRED);
+      wide += equal ? rounds(n) * longest : std::max(longest * key_us(n), keys * KEY_PAIRED / PLACES + behind * longest * KEY_PAIRED);
     } else {
       alone = std::max(alone, longest * KEY_NARROW);
       behind_narrow += (equal ? 0.25 : 0.5) * longest * KEY_NARROW;
@@ -377,6 +390,9 @@ static double attend_us(const PhaseSums (&s)[2], const AttendPhase (&ph)[2], dou
   const double merge = parts > 1 ? MERGE + parts / 16 + (wide > 0 ? 4 : 2) * pairs * parts * (ABSB_HEAD_DIM + 2) * 4 / BYTES_US : 0.0;
   return START + std::max(wide, narrow) + (alone > 0 ? 0.35 * std::min(wide, narrow) : 0.0) + 2 * units / PLACES + merge;
 }
+
+// Work-groups that a tail of tiles is cut into, at most: 68 MB of partial results.
+constexpr int TAIL_WGS = 1024;
 
 static int plan_attend(const absb_layer* layer, const absb_batch* batch, const absb_rows* rows, const absb_shared_prefix* shared,
                        const absb_score_opts* opts, bool any_options, AttendPlan* plan) {
@@ -448,8 +464,9 @@ static int plan_attend(const absb_layer* layer, const absb_batch* batch, const a
   seen.tiles = sums[1].tiles;
   // Both phases' keys are cut into stretches that take about equally long (a narrow tile's key takes half of a wide one's).
   const int64_t owners[2] = {shared ? shared->groups : 0, Bt};
-  const int64_t slots[2] = {(((int64_t)off[Bt] * G) >> tile[0]) + owners[0], (((int64_t)off[Bt] * G) >> tile[1]) + Bt};
-  auto work_groups = [&](const AttendPhase (&ph)[2]) { return (ph[0].slots * ph[0].splits + ph[1].slots * ph[1].splits) * Hkv; };
+  int64_t slots[2];
+  for (int i = 0; i < 2; ++i) slots[i] = owners[i] <= DENSE_OWNERS ? sums[i].tiles : (((int64_t)off[Bt] * G) >> tile[i]) + owners[i];
+  auto work_groups = [&](const AttendPhase (&ph)[2]) { return (ph[0].slots * ph[0].splits + ph[1].whole + (ph[1].slots - ph[1].whole) * ph[1].splits) * Hkv; };
   auto choose = [&](const PhaseSums (&s)[2], int most_splits) {
     double whole[2], best = 0;
     for (int i = 0; i < 2; ++i) whole[i] = s[i].max_keys * (tile[i] == 7 ? 2.0 : 1.0);
@@ -458,30 +475,54 @@ static int plan_attend(const absb_layer* layer, const absb_batch* batch, const a
       const double stretch = std::max(whole[0], whole[1]) / cuts;
       for (int i = 0; i < 2; ++i) ph[i] = cut_phase(s[i], tile[i], (int64_t)std::ceil(whole[i] / stretch - 1e-6), owners[i], slots[i]);
       if (ph[1].splits > most_splits || (cuts > 1 && work_groups(ph) > MAX_WGS)) break;
-      const double us = attend_us(s, ph, (double)p.rows * layer->num_q_heads, Hkv);
+      const double us = attend_us(s, ph, (double)p.rows * layer->num_q_heads, Hkv, 0);
       // (as good as level: fewer parts, unless they are those of narrow tiles, which are small)
       if (cuts > 1 && us >= (tile[0] == 7 || tile[1] == 7 ? 0.98 : 0.998) * best) continue;
       best = us;
       p.shared = ph[0];
       p.own = ph[1];
     }
+    // (About) equal wide tiles that fill the chip and a bit: those that are left over are cut, into at most TAIL_WGS work-groups (560
+    // tiles of 4096 capped scores: 250 us with none cut or all, 198; 640 of them without a cap 207 -> 198, 768 best as they are).
+    const int64_t places = 512 / Hkv, full = s[1].tiles / std::max<int64_t>(places, 1) * places, rest = s[1].tiles - full;
+    if (shared || tile[1] != 7 || !full || !rest || (rest + Bt) * Hkv * 32 > MAX_WGS || 20 * s[1].keys < 17.0 * s[1].tiles * s[1].max_keys) return;
+    AttendPhase ph[2] = {};
+    for (int cuts = 2; cuts <= 64 && rest * Hkv * cuts <= TAIL_WGS; ++cuts) {
+      ph[1] = cut_phase(s[1], 7, cuts, owners[1], slots[1]);
+      if (ph[1].splits != cuts) continue;
+      const double us = attend_us(s, ph, (double)p.rows * layer->num_q_heads, Hkv, full);
+      if (us >= 0.98 * best) continue;
+      best = us;
+      p.own = ph[1];
+      p.own.whole = full;
+    }
   };
-  int parts_any = 0;  // the most that any options make
+  int64_t parts_any = 0, tail_any = 0;  // the most that any options make: of all rows; partial results of a tail
   if (p.rows) {
     choose(sums, 1 << 30);
-    parts_any = p.shared.splits + p.own.splits;
+    parts_any = p.own.whole ? 1 : p.shared.splits + p.own.splits;
     if (!shared) {
       // a window may make more splits than there are without it, as many as fill the chip twice
-      const int64_t fill = ceil_div(1024, sums[1].tiles * Hkv);
-      parts_any = std::max(parts_any, (int)std::min<int64_t>(64, fill));
+      parts_any = std::max(parts_any, std::min<int64_t>(64, ceil_div(1024, sums[1].tiles * Hkv)));
+      if (tile[1] == 7 && sums[1].tiles * Hkv > 512) tail_any = TAIL_WGS * 128 + 64 * layer->num_q_heads;
     }
     if (bounded) {
       const PhaseSums windowed[2] = {PhaseSums{}, seen};
-      choose(windowed, parts_any);
+      choose(windowed, (int)parts_any);
     }
   }
   p.parts = p.shared.splits + p.own.splits;
-  const int ws_parts = any_options ? parts_any : p.parts;
+  p.cut_rows = p.rows;
+  if (p.own.whole) {  // tiles to slots: the last owners' are whole
+    int64_t left = p.own.whole, slot = slots[1];
+    for (int b = Bt - 1; left > 0; --b) {
+      const int64_t n = (off[b + 1] - off[b]) * (int64_t)G, tiles = n ? ((n - 1) >> 7) + 1 : 0, cut = std::max<int64_t>(tiles - left, 0);
+      left -= tiles - cut;
+      slot = Bt <= DENSE_OWNERS ? slot - (tiles - cut) : (((int64_t)off[b] * G) >> 7) + b + cut;
+      p.cut_rows = off[b] + ceil_div(cut * 128, G);
+    }
+    p.own.whole = slots[1] - slot;
+  }
   if (work_groups({p.shared, p.own}) > MAX_WGS) return ABSB_ERR_BAD_SHAPE;
   // Owners of one tile have their rows read once; what the last-level cache could not keep for the next call anyway passes it by.
   // Narrow: one token behind 128 K 101 -> 88 us, 64 behind 2 K 95 -> 84, 64 behind 1 K, 134 MB, 50.3 -> 44.7.  Wide: 12 behind 128 K
@@ -490,10 +531,11 @@ static int plan_attend(const absb_layer* layer, const absb_batch* batch, const a
   auto past = [&](int log2_tile, int64_t most_rows) { return most_rows * G <= int64_t(1) << log2_tile && mib >= (log2_tile == 7 ? 192 : 96); };
   p.shared.stream = past(tile[0], most);
   p.own.stream = past(tile[1], max_n);
-  const int64_t pairs = p.rows * layer->num_q_heads;
-  if (ws_parts > 1) {
-    p.ws_part_ml = align256((size_t)pairs * ws_parts * ABSB_HEAD_DIM * 4);
-    p.ws_bytes = p.ws_part_ml + align256((size_t)pairs * ws_parts * 2 * 4);
+  int64_t partial = p.parts > 1 ? p.cut_rows * layer->num_q_heads * p.parts : 0;
+  if (any_options) partial = std::max(parts_any > 1 ? p.rows * layer->num_q_heads * parts_any : 0, tail_any);
+  if (partial) {
+    p.ws_part_ml = align256((size_t)partial * ABSB_HEAD_DIM * 4);
+    p.ws_bytes = p.ws_part_ml + align256((size_t)partial * 2 * 4);
   }
   *plan = p;
   return ABSB_OK;

@@ -59,14 +59,25 @@ __device__ __forceinline__ float across_halves(float x, Op op) {
   return op(bitcast<float>(h[0]), bitcast<float>(h[1]));
 }
 
-// The owner of tile slot x: the largest o in [0, n) with slot0(o) <= x, where slot0(o) = row0(o) * G / tile + o, and its rows
-// [row0(o), row0(o + 1)).  The wave looks at 64 places at a time; up to 63 owners are one look.
+// The owner of tile slot x, its rows [row0(o), row0(o + 1)), its first slot.  Few owners: by a sum over their tiles.  Many: the largest
+// o in [0, n) with slot0(o) <= x, where slot0(o) = row0(o) * G / tile + o; the wave looks at 64 places at a time.
 struct Owner {
   int o, r0, r1, len;  // ... and lens[o]
+  int64_t slot0;
 };
 template <typename F>
 __device__ __forceinline__ Owner owner_of(int n, int64_t x, int G, int log2_tile, const int32_t* lens, F row0) {
   const int lane = threadIdx.x & 63;
+  if (n <= DENSE_OWNERS) {
+    const int r = row0(min(lane, n)), len = lens[min(lane, n - 1)];
+    const int next = __shfl(r, min(lane + 1, 63));
+    const uint32_t tiles = ((uint32_t)(next - r) * (uint32_t)G + (1u << log2_tile) - 1) >> log2_tile;
+    uint32_t total;
+    const uint32_t before = wave_incl_scan_u32(lane < n ? tiles : 0, &total) - (lane < n ? tiles : 0);
+    const int i = max(0, __popcll(__ballot(lane < n && (int64_t)before <= x)) - 1);
+    return Owner{i, __builtin_amdgcn_readlane(r, i), __builtin_amdgcn_readlane(r, i + 1), __builtin_amdgcn_readlane(len, i),
+                 __builtin_amdgcn_readlane((int)before, i)};
+  }
   int lo = 0, hi = n;  // the owner is in [lo, hi)
   while (hi - lo > 63) {
     const int step = (hi - lo + 63) >> 6, at = lo + lane * step;
@@ -77,7 +88,8 @@ __device__ __forceinline__ Owner owner_of(int n, int64_t x, int G, int log2_tile
   const int at = min(lo + lane, hi), r = row0(at), len = lens[min(at, n - 1)];
   const uint64_t below = __ballot(lo + lane < hi && (((int64_t)r * G) >> log2_tile) + at <= x);
   const int i = max(0, __popcll(below) - 1);
-  return Owner{lo + i, __builtin_amdgcn_readlane(r, i), __builtin_amdgcn_readlane(r, i + 1), __builtin_amdgcn_readlane(len, i)};
+  const int r0 = __builtin_amdgcn_readlane(r, i);
+  return Owner{lo + i, r0, __builtin_amdgcn_readlane(r, i + 1), __builtin_amdgcn_readlane(len, i), (((int64_t)r0 * G) >> log2_tile) + lo + i};
 }
 // The shared tokens of request b: those of the last group g with first[g] <= b.  `first`, `len`: the lane's group of the first 64,
 // asked for beforehand.
@@ -469,14 +481,16 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) 
   const bool shared = blockIdx.x < p.shared_units;
   const uint32_t unit = shared ? blockIdx.x : blockIdx.x - p.shared_units;
   const AttendPhase& ph = shared ? p.shared : p.own;
-  const int owners = ph.owners, splits = ph.splits, log2_tile = ph.log2_tile, chunk = ph.chunk;
+  const int owners = ph.owners, splits = ph.splits, log2_tile = ph.log2_tile;
   const bool stream = ph.stream;
   const int part0 = shared ? 0 : p.shared.splits;
   const bool wide = log2_tile == 7;
   const int kv_head = (int)(unit % (uint32_t)p.Hkv);
   const uint32_t rest = unit / (uint32_t)p.Hkv;
-  const int split = (int)(rest % (uint32_t)splits);
-  const int64_t slot = ph.slots - 1 - (int64_t)(rest / (uint32_t)splits);
+  const bool cut = (int64_t)rest >= ph.whole;
+  const uint32_t among = cut ? rest - (uint32_t)ph.whole : 0;
+  const int split = (int)(among % (uint32_t)splits);
+  const int64_t slot = ph.slots - 1 - (cut ? ph.whole + (int64_t)(among / (uint32_t)splits) : (int64_t)rest);
   int group_first = 0, group_len = 0;
   if (!shared && p.groups) {
     const int mine = min(lane, p.groups - 1);
@@ -489,7 +503,7 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) 
   t.r0 = own.r0;
   t.n = own.r1 - own.r0;
   // (an owner's pairs are fewer than 2^31: absb_attend_* sees to it)
-  const uint32_t f0 = (uint32_t)(slot - (((int64_t)t.r0 * p.G >> log2_tile) + owner)) << log2_tile;
+  const uint32_t f0 = (uint32_t)(slot - own.slot0) << log2_tile;
   t.pairs = (int)((uint32_t)t.n * (uint32_t)p.G - f0);
   if (t.pairs <= 0) return;
   t.tok0 = (int)(f0 / (uint32_t)p.G);
@@ -526,7 +540,8 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) 
     for (int j = 0; j < 16; ++j) st.o[i][j] = 0.0f;
 
   // ---- the split's keys [begin, end)
-  const int64_t from = ((int64_t)tile_lo & ~int64_t(63)) + (int64_t)split * chunk;
+  const int64_t chunk = cut ? ph.chunk : int64_t(1) << 31;
+  const int64_t from = ((int64_t)tile_lo & ~int64_t(63)) + split * chunk;
   const int begin = (int)min(from, (int64_t)tile_hi + 1);
   const int end = (int)min(from + chunk, (int64_t)tile_hi + 1);
   if (begin < end) {
@@ -679,7 +694,7 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) 
   }
   st.l = across_halves(st.l, [](float a, float b) { return a + b; });
 
-  const bool one = p.parts == 1, none = !one && begin >= end;  // (a split without keys has weight 0: its sum says so)
+  const bool one = p.parts == 1 || !cut, none = !one && begin >= end;  // (a split without keys has weight 0: its sum says so)
   const int half = lane >> 5;
   auto put_sums = [&](int64_t at, float m, float l) __attribute__((always_inline)) {
     if (!one)
@@ -749,11 +764,22 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) 
   }
 }
 
-// The parts of a (row, query head), a wave each: half a wave a part, a lane four channels.
-template <int DT>
-__global__ __launch_bounds__(256) void attend_merge_kernel(AttendParams p, int64_t pairs) {
+// The parts of a (row, query head), a wave each: half a wave a part, a lane four channels.  TAIL: of the first `n` tile slots only, a
+// wave a row of a tile; else of the first `n` pairs.
+template <int DT, bool TAIL>
+__global__ __launch_bounds__(256) void attend_merge_kernel(AttendParams p, int64_t n) {
   const int lane = threadIdx.x & 63, half = lane >> 5;
-  for (int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); at < pairs; at += (int64_t)gridDim.x * 4) {
+  int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (TAIL) {
+    const int log2_tile = p.own.log2_tile, i = (int)(at & ((1 << log2_tile) - 1));
+    const uint32_t unit = (uint32_t)(at >> log2_tile);
+    const int64_t slot = unit / (uint32_t)p.Hkv;
+    const Owner own = owner_of(p.own.owners, slot, p.G, log2_tile, p.seq_lens, [&](int o) { return p.row_off[o]; });
+    const uint32_t pair = ((uint32_t)(slot - own.slot0) << log2_tile) + (uint32_t)i;
+    if (pair >= (uint32_t)(own.r1 - own.r0) * (uint32_t)p.G) return;
+    at = (int64_t)(own.r0 + (int)(pair / (uint32_t)p.G)) * p.Hq + (int)(unit % (uint32_t)p.Hkv) * p.G + (int)(pair % (uint32_t)p.G);
+  }
+  for (; TAIL || at < n; at += (int64_t)gridDim.x * 4) {
     const float* ml = p.part_ml + at * p.parts * 2;
     const float* o = p.part_o + at * p.parts * ABSB_HEAD_DIM + 4 * (lane & 31);
     constexpr int TRIP = 16;  // parts fetched at once
@@ -790,17 +816,21 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(AttendParams p, int64
     if (half == 0)
       *reinterpret_cast<uint2*>(p.out + at * ABSB_HEAD_DIM + 4 * lane) = uint2{pack2<DT>(x[0] * inv, x[1] * inv), pack2<DT>(x[2] * inv, x[3] * inv)};
     if (p.lse && lane == 0) p.lse[at] = L == 0.0f ? -__builtin_inff() : (M + __builtin_log2f(L)) * LN2;
+    if (TAIL) return;
   }
 }
 
 template <int DT, int CAP, bool BIAS>
 static void launch_parts(const AttendParams& p, int64_t rows, hipStream_t stream) {
-  const int64_t own_units = p.own.slots * p.Hkv * p.own.splits;
+  const int64_t own_units = (p.own.whole + (p.own.slots - p.own.whole) * p.own.splits) * p.Hkv;
   hipLaunchKernelGGL((attend_kernel<DT, CAP, BIAS>), dim3((unsigned)(p.shared_units + own_units)), dim3(ATT_THREADS), 0, stream, p);
-  if (p.parts > 1) {
+  if (p.parts > 1 && p.own.whole) {
+    const int64_t slots = p.own.slots - p.own.whole;
+    hipLaunchKernelGGL((attend_merge_kernel<DT, true>), dim3((unsigned)((slots * p.Hkv << p.own.log2_tile) / 4)), dim3(256), 0, stream, p, slots);
+  } else if (p.parts > 1) {
     const int64_t pairs = rows * p.Hq;
     const unsigned grid = (unsigned)std::min<int64_t>((pairs + 3) / 4, MAX_WGS);
-    hipLaunchKernelGGL((attend_merge_kernel<DT>), dim3(grid), dim3(256), 0, stream, p, pairs);
+    hipLaunchKernelGGL((attend_merge_kernel<DT, false>), dim3(grid), dim3(256), 0, stream, p, pairs);
   }
 }
 template <int DT, int CAP>

@@ -545,6 +545,22 @@ def test_attend_past_the_caches(lens, new, shared):
     Call(lens, new, 32, 8, 64, shared=shared, seed=5).check(f"{lens} {new} {shared}")
 
 
+@pytest.mark.parametrize("lens,new,Hq,Hkv,opts", [
+    ([9100], [1153], 64, 64, dict(window=5000)),                                  # 10 tiles a head, places for 8
+    ([9000, 30, 9100, 9050, 9040], [300, 0, 1, 0, 480], 96, 32, dict(window=6011)),   # groups of three across the cut
+    ([9000, 8990], [45, 850], 80, 16, dict(softcap=30.0, window=4000)),
+    ([30000, 29990], [2600, 2030], 16, 16, dict(slopes=True)),
+    ([30000], [1200], 64, 32, dict()),
+])
+def test_attend_of_equal_tiles_that_fill_the_chip_and_a_bit(lens, new, Hq, Hkv, opts):
+    for dt in ("f16", "bf16"):
+        c = Call(lens, new, Hq, Hkv, 16, dt, seed=9, **opts)
+        n = c.ws.numel() - 256
+        c.ws, guard = c.ws[:n], c.ws[n:]
+        c.check(f"{lens} {new} {Hq}/{Hkv} {dt} {opts}")
+        assert (guard == 0xA5).all()
+
+
 def test_attend_of_more_than_64_parts():
     absb = _absb()
     c = Call([120001], [1], 8, 1, 64, "f16", shared=[60032])
