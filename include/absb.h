@@ -15,6 +15,9 @@
  *            from a paged KV cache through the page table (Sec. 3.4, kernel 3), as
  *            split-K partials merged by log-sum-exp
  *
+ * and what a server does around that path on the same paged cache: the rows of a step and their pages, rotary
+ * positions with the cache write, dense attention of new rows, also behind a prefix that requests share.
+ *
  * Conventions
  *   - Every function returns ABSB_OK (0) or a negative absb_status.  No exceptions, no exit.
  *   - Host-visible arguments are validated before anything is launched; on error nothing

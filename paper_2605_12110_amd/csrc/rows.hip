@@ -16,8 +16,9 @@ namespace absb {
 // read here: a row in a fresh page takes it from the ring, not from the table.  The cursors change at the end of the call only,
 // written by the work-group that finishes last, since until then others may be reading them.
 //
-// Bound by latency: lengths in, page table or ring in, rows out, and two barriers between.  256 threads while they cover the batch
-// (64 requests: 5.6 us with 1024, 16 waves at every barrier), else 1024.
+// Bound by latency: lengths in, page table or ring in, rows out, and two barriers between.  As few threads as cover the batch: a
+// barrier costs by its waves (64 requests, a token each: 3.4, 3.6 and 4.8 us with 256, 512 and 1024 threads), a second round over
+// the batch more (300: 7.2, 5.2, 6.3; 600: 9.2, 8.8, 6.3; 2000: 17.5, 12.8, 12.7).
 struct MapSums {
   int32_t rows, take, give;  // of the requests before a point
 };
@@ -197,7 +198,8 @@ int launch_map_rows(const MapParams& p, hipStream_t stream) {
 // of a million radians is off by 0.03.  Its upper 32 bits, as a number in [-1/2, 1/2), go to the hardware's sine and cosine
 // of turns (off by at most 1.3e-7 over that range, where a 16-bit result is off by 2^-12 at best).
 //
-// Bound by memory: (Hq + 2 Hkv) rows of 256 bytes in and out a token.  A lane holds 16-byte pieces (of both halves of a pair's
+// Bound by memory: (Hq + 2 Hkv) rows of 256 bytes in and out a token (8192 tokens of 48 heads 38.5 us, 32 K 140 us, 5.2 and 5.65 TB/s;
+// 16 tokens 4.0 us, a chain of round trips).  A lane holds 16-byte pieces (of both halves of a pair's
 // channels), LANES of them a head; a wave works on one token and a stretch of its heads, so that the sines are worked out once for
 // several heads.
 __device__ __forceinline__ uint64_t turns_of(double f) {
@@ -365,7 +367,8 @@ int launch_rotate(RotateParams p, int dtype, hipStream_t stream) {
   // lanes a head: the pieces that pass beside the pairs of pieces that turn, up to a power of two (8 when all channels turn)
   const int lanes = p.rot % (p.halves ? 16 : 8) ? 64 : p.halves && p.rot == ABSB_HEAD_DIM ? 8 : 16;
   const int heads = p.nq + 2 * p.nkv, at_once = 64 / lanes;
-  // few tokens: a wave takes as many heads as it holds at once; many: a token
+  // few tokens: a wave takes as many heads as it holds at once; many: a token (48 heads, 64 tokens: 3.5 us, and 5.6 with a token a
+  // wave; 700: both 6.6; 2048: 15.9 and 9.9)
   p.parts = (heads + at_once - 1) / at_once;
   if ((int64_t)p.n_rows * p.parts > 8192) p.parts = 1;
   p.heads_per_part = ((heads + p.parts - 1) / p.parts + at_once - 1) / at_once * at_once;
