@@ -519,7 +519,15 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) 
   const int own_from = !shared && p.groups ? shared_tokens(p, owner, group_first, group_len) : 0;
 
   const RowOf row = row_of(p, t, shared, own_from, owner, kv_head, (wide ? 32 * wave : 0) + (lane & 31));
-  const bool valid = row.row >= 0, sees = valid && row.lo <= row.hi;
+  const bool valid = row.row >= 0;
+  // (asked for ahead of what the keys wait for: tiles of a few keys 63.6 -> 61.0 us of 2560, 12.2 -> 11.8 us of a small step)
+  u32x4 q[8];
+#pragma unroll
+  for (int c = 0; c < 8; ++c) {
+    q[c] = u32x4{0u, 0u, 0u, 0u};
+    if (valid) q[c] = *reinterpret_cast<const u32x4*>(p.q + ((int64_t)row.row * p.Hq + row.head) * ABSB_HEAD_DIM + (2 * c + (lane >> 5)) * 8);
+  }
+  const bool sees = valid && row.lo <= row.hi;
   const int lo = sees ? row.lo : INT32_MAX, hi = sees ? row.hi : -1;
   auto lesser = [](uint32_t a, uint32_t b) { return a < b ? a : b; };
   auto greater = [](uint32_t a, uint32_t b) { return a > b ? a : b; };
@@ -551,12 +559,6 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) 
   const int begin = (int)min(from, (int64_t)tile_hi + 1);
   const int end = (int)min(from + chunk, (int64_t)tile_hi + 1);
   if (begin < end) {
-    u32x4 q[8];
-#pragma unroll
-    for (int c = 0; c < 8; ++c) {
-      q[c] = u32x4{0u, 0u, 0u, 0u};
-      if (valid) q[c] = *reinterpret_cast<const u32x4*>(p.q + ((int64_t)row.row * p.Hq + row.head) * ABSB_HEAD_DIM + (2 * c + (lane >> 5)) * 8);
-    }
     const float slope_log2 = BIAS && valid ? p.slopes[row.head] * LOG2E : 0.0f;
     const int32_t* pages = p.page_table + (int64_t)t.table_row * p.pt_stride;
     const char *kb = p.k + kv_head * p.s_head, *vb = p.v + kv_head * p.s_head;
