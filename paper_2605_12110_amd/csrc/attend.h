@@ -18,7 +18,7 @@ struct AttendPhase {
   int32_t owners;
   int32_t log2_tile;  // rows (token, query head of the group) of a work-group: 128, or 32 that its four waves share
   int32_t splits;  // of a tile's keys, a work-group each
-  int32_t chunk;   // keys of a split, a multiple of 128
+  int32_t chunk;   // keys of a split of the longest tile, a multiple of 128; a tile's own are divided evenly
   int32_t stream;  // 1: rows are read past the caches
   int64_t slots;   // tiles, empty ones included
   int64_t whole;   // of them, the last: not cut, their results written straight to the output.  (All cut or none, but for equal

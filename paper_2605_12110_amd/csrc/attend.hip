@@ -35,6 +35,7 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int ATT_THREADS = 256, ATT_WAVES = 4;
+constexpr int LEAST_KEYS = 256;  // of a split, if it is planned to have as many
 constexpr int ROW_BYTES = ABSB_HEAD_DIM * 2;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
@@ -554,8 +555,12 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) 
     for (int j = 0; j < 16; ++j) st.o[i][j] = 0.0f;
 
   // ---- the split's keys [begin, end)
-  const int64_t chunk = cut ? ph.chunk : int64_t(1) << 31;
-  const int64_t from = ((int64_t)tile_lo & ~int64_t(63)) + split * chunk;
+  // The tile's keys are divided evenly: windows and documents leave it fewer than the host has planned for, and some requests are short
+  // (twice 32 tokens of documents of 1900 behind 34 K: 44 us in stretches as planned, 18.6; 8 tokens behind 4 to 32 K 107, 104).
+  const int first = tile_lo & ~63;
+  const uint32_t keys = tile_lo <= tile_hi ? (uint32_t)(tile_hi + 1 - first) : 0;
+  const int64_t chunk = cut ? max(min((uint32_t)LEAST_KEYS, (uint32_t)ph.chunk), ((keys + splits - 1) / (uint32_t)splits + 127) & ~127u) : int64_t(1) << 31;
+  const int64_t from = (int64_t)first + split * chunk;
   const int begin = (int)min(from, (int64_t)tile_hi + 1);
   const int end = (int)min(from + chunk, (int64_t)tile_hi + 1);
   if (begin < end) {
