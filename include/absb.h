@@ -526,7 +526,8 @@ ABSB_API int absb_attend_workspace(const absb_layer* layer, const absb_batch* ba
  * host twin, row_off (and groups) are the same, and each is at least its rows (and its group's shared tokens beside them).  Slots beyond a
  * context may hold anything; the tokens of a context must be finite, also those that the row does not see.
  * Accumulation, maxima and sums are binary32; the softmax weights enter the product with V rounded to the K/V
- * type, their sum is taken before rounding. */
+ * type, and the output is divided by their sum as rounded: it stays a convex combination of value rows.  lse is of the sum
+ * before rounding. */
 ABSB_API int absb_attend_rows(const absb_layer* layer, const absb_batch* batch, const absb_rows* rows, const void* q,
                               const void* k_cache, const void* v_cache, void* out, float* lse,
                               const absb_score_opts* opts, void* workspace, size_t workspace_bytes, void* stream);

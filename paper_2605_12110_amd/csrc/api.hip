@@ -387,7 +387,7 @@ static double attend_us(const PhaseSums (&s)[2], const AttendPhase (&ph)[2], dou
     }
   }
   const double narrow = std::max(alone, bytes / BYTES_US * uneven + behind_narrow);
-  const double merge = parts > 1 ? MERGE + parts / 16 + (wide > 0 ? 4 : 2) * pairs * parts * (ABSB_HEAD_DIM + 2) * 4 / BYTES_US : 0.0;
+  const double merge = parts > 1 ? MERGE + parts / 16 + (wide > 0 ? 4 : 2) * pairs * parts * (ABSB_HEAD_DIM + 3) * 4 / BYTES_US : 0.0;
   return START + std::max(wide, narrow) + (alone > 0 ? 0.35 * std::min(wide, narrow) : 0.0) + 2 * units / PLACES + merge;
 }
 
@@ -536,7 +536,7 @@ static int plan_attend(const absb_layer* layer, const absb_batch* batch, const a
   if (any_options) partial = std::max(parts_any > 1 ? p.rows * layer->num_q_heads * parts_any : 0, tail_any);
   if (partial) {
     p.ws_part_ml = align256((size_t)partial * ABSB_HEAD_DIM * 4);
-    p.ws_bytes = p.ws_part_ml + align256((size_t)partial * 2 * 4);
+    p.ws_bytes = p.ws_part_ml + align256((size_t)partial * sizeof(PartSums));
   }
   *plan = p;
   return ABSB_OK;

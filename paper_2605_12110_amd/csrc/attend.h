@@ -25,6 +25,11 @@ struct AttendPhase {
                    // tiles that fill the chip and a bit: then the few that would have it to themselves afterwards are.)
 };
 
+// Of a partial result: maximum in log2 units, sums of the weights as rounded for the product with V and before rounding.
+struct PartSums {
+  float m, l, lx;
+};
+
 struct AttendPlan {
   AttendPhase shared, own;  // shared.owners = 0: no such phase
   int32_t parts;            // partial results of a row: shared.splits + own.splits
@@ -43,7 +48,7 @@ struct AttendParams {
   uint16_t* out;
   float* lse;
   float* part_o;   // [cut rows][Hq][parts][128], not normalised
-  float* part_ml;  // [cut rows][Hq][parts][2]: maximum in log2 units, sum
+  float* part_ml;  // [cut rows][Hq][parts] PartSums
   int64_t s_page, s_head, s_tok;  // bytes
   int32_t groups, pt_stride, Hq, Hkv, G, log2_page;
   int32_t inv_G;                  // 2^16 / G, rounded up

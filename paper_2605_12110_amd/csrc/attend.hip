@@ -130,8 +130,11 @@ struct Tile {
 };
 
 // Softmax state and output of a wave's 32 rows: lane l holds row l % 32; O[t][i] is channel 32 t + 8 (i / 4) + 4 (l / 32) + i % 4.
+// Two sums of weights: `l` as rounded for the product with V, by which the output is divided (it stays a convex combination of
+// value rows: with one dominant key, or many equal ones, all of the mass rounds the same way, and an output divided by the
+// other sum would be off by up to 2^-8 in bf16); `lx` before rounding, of which the log-sum is made.
 struct State {
-  float m, l;
+  float m, l, lx;
   f32x16 o[4];
 };
 
@@ -198,8 +201,9 @@ __device__ __forceinline__ void adjust(const AttendParams& p, f32x16 (&s)[KT], i
 }
 
 // The maximum that the rows' weights are taken against.  It follows the scores' own only when they exceed it by 2^RISE:
-// weights then reach 2^RISE, which the K/V types hold as exactly as those below 1, and the output is hardly ever scaled again
-// (with the true maximum some of a wave's 32 rows has a new one in most blocks).
+// weights then reach 2^RISE, which the K/V types hold to the same relative step as those below 1 (and the output is divided by
+// their sum as rounded), and the output is hardly ever scaled again (with the true maximum some of a wave's 32 rows has a new
+// one in most blocks).
 constexpr float RISE = 8.0f;
 template <int KT>
 __device__ __forceinline__ float largest(const f32x16 (&s)[KT]) {
@@ -222,6 +226,7 @@ __device__ __forceinline__ float new_maximum(const AttendParams& p, float mx, St
     const bool some = __any(st.m != -__builtin_inff());  // (else the output is still zero)
     st.m = mn;
     st.l *= alpha;
+    st.lx *= alpha;
     if (some) {
 #pragma unroll
       for (int t = 0; t < 4; ++t) st.o[t] *= alpha;
@@ -230,10 +235,16 @@ __device__ __forceinline__ float new_maximum(const AttendParams& p, float mx, St
   return st.m == -__builtin_inff() ? 0.0f : st.m;  // nothing seen yet: weights 0, not NaN
 }
 
-// Weights of the scores, rounded to the K/V type (two to a word: P^T as the product takes it), and their sum before rounding.
+// Two rounded weights onto a sum in binary32.
+template <int DT>
+__device__ __forceinline__ float add_pair(uint32_t w, float sum) {
+  return Elem<DT>::dot2(w, DT == ABSB_F16 ? 0x3c003c00u : 0x3f803f80u, sum);
+}
+
+// Weights of the scores, rounded to the K/V type (two to a word: P^T as the product takes it), and their sums.
 template <int DT, bool SCALED, int KT>
 __device__ __forceinline__ void weigh(const AttendParams& p, const f32x16 (&s)[KT], float base, u32x4 (&w)[2 * KT], State& st) {
-  float sum = 0.0f;
+  float sum = 0.0f, rounded = 0.0f;
 #pragma unroll
   for (int c = 0; c < 2 * KT; ++c)
 #pragma unroll
@@ -244,8 +255,10 @@ __device__ __forceinline__ void weigh(const AttendParams& p, const f32x16 (&s)[K
       sum += x;
       sum += y;
       w[c][j] = pack2<DT>(x, y);
+      rounded = add_pair<DT>(w[c][j], rounded);
     }
-  st.l += sum;
+  st.l += rounded;
+  st.lx += sum;
 }
 
 // O^T += V^T P^T for the 32 KT keys whose V rows are at `vl`.
@@ -271,7 +284,7 @@ __device__ __forceinline__ void add_values(const char* vl, const u32x4 (&w)[2 * 
 // The main part of a step of a wide tile, in an order of its own (the compiler's would wait for every read of LDS right before its
 // product): 16 products of the next block's scores, then 16 of this block's weights with its values; beside each, the vector work
 // of one score or two, and the read that the fourth product after it needs.  A product takes the matrix unit 32 cycles, an
-// exponential the vector unit 16, its other work 12.  `mx`: the largest of a lane's next scores; `away`: of the row from their
+// exponential the vector unit 16, its other work 12 and half an instruction of the rounded sum (which cost 3 % of a 4096-token prompt).  `mx`: the largest of a lane's next scores; `away`: of the row from their
 // first key.
 template <int DT, int CAP, bool BIAS>
 __device__ __forceinline__ void wide_step(const AttendParams& p, const char* kl, const char* vl, const u32x4 (&q)[8], const f32x16 (&s)[2],
@@ -280,7 +293,7 @@ __device__ __forceinline__ void wide_step(const AttendParams& p, const char* kl,
   constexpr int AHEAD = 4, SLOTS = 32;
   const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5, i16 = lane & 15, grp = (lane >> 4) & 1;
   u32x4 f[AHEAD], w[4];
-  float x = 0.0f, sum0 = 0.0f, sum1 = 0.0f;
+  float x = 0.0f, sum = 0.0f, rounded = 0.0f;
   mx = -__builtin_inff();
   auto fetch = [&](int j) __attribute__((always_inline)) {  // the operand of product j
     if (j < 16) {
@@ -313,11 +326,11 @@ __device__ __forceinline__ void wide_step(const AttendParams& p, const char* kl,
     for (int e = j * 8 / 7; e < (j + 1) * 8 / 7 && e < 32; ++e) {
       const float a = s[e >> 4][e & 15];
       const float y = exp2_fast(SCALED ? a - base : __builtin_fmaf(a, p.scale_log2, -base));
+      sum += y;
       if (e & 1) {
-        sum1 += y;
         w[e >> 3][(e & 7) >> 1] = pack2<DT>(x, y);
+        rounded = add_pair<DT>(w[e >> 3][(e & 7) >> 1], rounded);
       } else {
-        sum0 += y;
         x = y;
       }
     }
@@ -331,11 +344,12 @@ __device__ __forceinline__ void wide_step(const AttendParams& p, const char* kl,
         mx = fmaxf(mx, y);
       }
     }
-    asm volatile("" : "+v"(sum0), "+v"(sum1));  // (the sums are made here, not out of 32 kept values at the end)
+    asm volatile("" : "+v"(sum), "+v"(rounded));  // (the sums are made here, not out of 32 kept values at the end)
     __builtin_amdgcn_sched_barrier(0);
   }
   __builtin_amdgcn_s_setprio(0);
-  st.l += sum0 + sum1;
+  st.l += rounded;
+  st.lx += sum;
 }
 
 __device__ __forceinline__ uint64_t lane_u64(uint64_t v, int lane) {
@@ -478,7 +492,7 @@ static_assert(ATT_LDS >= 65536 && 2 * (ATT_LDS + 2048) <= 160 * 1024, "two work-
 template <int DT, int CAP, bool BIAS>
 __global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) {
   __shared__ __align__(16) char s_kv[ATT_LDS];
-  __shared__ float s_ml[ATT_WAVES][2][32];
+  __shared__ float s_ml[ATT_WAVES][3][32];
   __shared__ int s_lo[ATT_WAVES], s_hi[ATT_WAVES];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   fetch_arguments<0, sizeof(AttendParams)>();  // (what follows is a chain of round trips; the arguments make one of it)
@@ -548,7 +562,7 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) 
   }
   State st;
   st.m = -__builtin_inff();
-  st.l = 0.0f;
+  st.l = st.lx = 0.0f;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -706,14 +720,15 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) 
     }
   }
   st.l = across_halves(st.l, [](float a, float b) { return a + b; });
+  st.lx = across_halves(st.lx, [](float a, float b) { return a + b; });
 
   const bool one = p.parts == 1 || !cut, none = !one && begin >= end;  // (a split without keys has weight 0: its sum says so)
   const int half = lane >> 5;
-  auto put_sums = [&](int64_t at, float m, float l) __attribute__((always_inline)) {
+  auto put_sums = [&](int64_t at, float m, float l, float lx) __attribute__((always_inline)) {
     if (!one)
-      *reinterpret_cast<float2*>(p.part_ml + (at * p.parts + part0 + split) * 2) = make_float2(m, l);
+      reinterpret_cast<PartSums*>(p.part_ml)[at * p.parts + part0 + split] = PartSums{m, l, lx};
     else if (p.lse)
-      p.lse[at] = l == 0.0f ? -__builtin_inff() : (m + __builtin_log2f(l)) * LN2;
+      p.lse[at] = lx == 0.0f ? -__builtin_inff() : (m + __builtin_log2f(lx)) * LN2;
   };
   auto put = [&](int64_t at, int ch, f32x4 o, float inv) __attribute__((always_inline)) {
     if (one)
@@ -725,7 +740,7 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) 
     if (!valid) return;
     const int64_t at = (int64_t)row.row * p.Hq + row.head;
     const float inv = st.l == 0.0f ? 0.0f : 1.0f / st.l;
-    if (half == 0) put_sums(at, st.m, st.l);
+    if (half == 0) put_sums(at, st.m, st.l, st.lx);
     if (none) return;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -742,6 +757,7 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) 
     if (half == 0) {
       s_ml[wave][0][col] = st.m;
       s_ml[wave][1][col] = st.l;
+      s_ml[wave][2][col] = st.lx;
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -755,7 +771,7 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) 
   if (r >= t.pairs) return;
   const PairOf pair = pair_of_tile(p, t, r);
   const int64_t at = (int64_t)(t.r0 + pair.tok) * p.Hq + kv_head * p.G + pair.g;
-  float m = -__builtin_inff(), l = 0.0f, w[ATT_WAVES];
+  float m = -__builtin_inff(), l = 0.0f, lx = 0.0f, w[ATT_WAVES];
 #pragma unroll
   for (int x = 0; x < ATT_WAVES; ++x) m = fmaxf(m, s_ml[x][0][r]);
   const float base = m == -__builtin_inff() ? 0.0f : m;
@@ -763,8 +779,9 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) 
   for (int x = 0; x < ATT_WAVES; ++x) {
     w[x] = exp2_fast(s_ml[x][0][r] - base);
     l = __builtin_fmaf(s_ml[x][1][r], w[x], l);
+    lx = __builtin_fmaf(s_ml[x][2][r], w[x], lx);
   }
-  if (c == 0) put_sums(at, m, l);
+  if (c == 0) put_sums(at, m, l, lx);
   if (none) return;
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
@@ -775,6 +792,12 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attend_kernel(AttendParams p) 
     for (int x = 0; x < ATT_WAVES; ++x) o += *reinterpret_cast<const f32x4*>(s_o + (x * 32 + r) * NARROW_PITCH + ch) * w[x];
     put(at, ch, o, inv);
   }
+}
+
+__device__ __forceinline__ float wave_sum(float x) {
+  x = row16_sum(x);
+  return bitcast<float>(__builtin_amdgcn_readlane(bitcast<int>(x), 0)) + bitcast<float>(__builtin_amdgcn_readlane(bitcast<int>(x), 16)) +
+         bitcast<float>(__builtin_amdgcn_readlane(bitcast<int>(x), 32)) + bitcast<float>(__builtin_amdgcn_readlane(bitcast<int>(x), 48));
 }
 
 // The parts of a (row, query head), a wave each: half a wave a part, a lane four channels.  TAIL: of the first `n` tile slots only, a
@@ -793,19 +816,20 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(AttendParams p, int64
     at = (int64_t)(own.r0 + (int)(pair / (uint32_t)p.G)) * p.Hq + (int)(unit % (uint32_t)p.Hkv) * p.G + (int)(pair % (uint32_t)p.G);
   }
   for (; TAIL || at < n; at += (int64_t)gridDim.x * 4) {
-    const float* ml = p.part_ml + at * p.parts * 2;
+    const PartSums* sums = reinterpret_cast<const PartSums*>(p.part_ml) + at * p.parts;
     const float* o = p.part_o + at * p.parts * ABSB_HEAD_DIM + 4 * (lane & 31);
     constexpr int TRIP = 16;  // parts fetched at once
-    float M = -__builtin_inff(), L = 0.0f;
+    float M = -__builtin_inff(), L = 0.0f, Lx = 0.0f;
     f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int i0 = 0; i0 < p.parts; i0 += 64) {
-      float2 mine = make_float2(-__builtin_inff(), 0.0f);
-      if (i0 + lane < p.parts) mine = *reinterpret_cast<const float2*>(ml + (i0 + lane) * 2);
-      if (mine.y == 0.0f) mine.x = -__builtin_inff();  // (a NaN stays one)
-      const float top = fmaxf(M, wave_max_f32(mine.x)), base = top == -__builtin_inff() ? 0.0f : top;
-      const float a = exp2_fast(M - base), w = exp2_fast(mine.x - base);
+      PartSums mine = {-__builtin_inff(), 0.0f, 0.0f};
+      if (i0 + lane < p.parts) mine = sums[i0 + lane];
+      if (mine.l == 0.0f) mine.m = -__builtin_inff();  // (a NaN stays one)
+      const float top = fmaxf(M, wave_max_f32(mine.m)), base = top == -__builtin_inff() ? 0.0f : top;
+      const float a = exp2_fast(M - base), w = exp2_fast(mine.m - base);
       M = top;
-      L = __builtin_fmaf(L, a, mine.y * w);  // (a lane's own parts)
+      L = __builtin_fmaf(L, a, mine.l * w);  // (a lane's own parts)
+      Lx = __builtin_fmaf(Lx, a, mine.lx * w);
       x *= a;
       const int n = min(64, p.parts - i0);
       for (int i = 0; i < n; i += TRIP) {
@@ -822,13 +846,12 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(AttendParams p, int64
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) x[j] = across_halves(x[j], [](float a, float b) { return a + b; });
-    L = row16_sum(L);
-    L = bitcast<float>(__builtin_amdgcn_readlane(bitcast<int>(L), 0)) + bitcast<float>(__builtin_amdgcn_readlane(bitcast<int>(L), 16)) +
-        bitcast<float>(__builtin_amdgcn_readlane(bitcast<int>(L), 32)) + bitcast<float>(__builtin_amdgcn_readlane(bitcast<int>(L), 48));
+    L = wave_sum(L);
+    Lx = wave_sum(Lx);
     const float inv = L == 0.0f ? 0.0f : 1.0f / L;
     if (half == 0)
       *reinterpret_cast<uint2*>(p.out + at * ABSB_HEAD_DIM + 4 * lane) = uint2{pack2<DT>(x[0] * inv, x[1] * inv), pack2<DT>(x[2] * inv, x[3] * inv)};
-    if (p.lse && lane == 0) p.lse[at] = L == 0.0f ? -__builtin_inff() : (M + __builtin_log2f(L)) * LN2;
+    if (p.lse && lane == 0) p.lse[at] = Lx == 0.0f ? -__builtin_inff() : (M + __builtin_log2f(Lx)) * LN2;
     if (TAIL) return;
   }
 }

@@ -793,3 +793,27 @@ def test_the_run_of_a_server():
             assert (sparse.double() - out.double()).abs().max() <= 4 * STEP["f16"] * float(vn.abs().max().double().clamp(min=4.0)) * 1.5
             assert (sparse_lse - lse).abs().max() <= 2e-4
         lens = now
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("lens,new,shared,opts", [
+    ([700], [600], None, dict()), ([700], [600], None, dict(softcap=50.0)), ([700], [600], None, dict(slopes=True)),   # wide tiles
+    ([900], [4], None, dict()), ([9000], [4], None, dict()), ([9000], [300], None, dict(softcap=50.0)),                  # narrow; in parts
+    ([1100, 1300], [2, 3], [1024], dict()),
+])
+def test_attend_outputs_stay_weighted_means(dt, lens, new, shared, opts):
+    """The same values at every key: their mean, whatever the weights.  One key in 32 has a score above the others', by 2^0 to 2^8 from
+    row to row, so that nearly all of the mass rounds the same way; that must not move the mean.  Sums of n <= 9000 weights in
+    binary32, in chains of at most n / 16, are off by n / 16 * 2^-24 < 2^-14 on either side, less than half a step of the values
+    (2^-12 and 2^-9, relatively): every output rounds to the value itself."""
+    torch = _torch()
+    c = Call(lens, new, 8, 2, 16, dt, shared=shared, seed=7, **opts)
+    for b, L in enumerate(lens):
+        t = np.arange(L)
+        page, slot = torch.from_numpy(c.table_host[b, t // 16].astype(np.int64)).cuda(), torch.from_numpy(t % 16).cuda()
+        c.view(c.k)[page, :, slot] = torch.from_numpy((t % 32 == 0) * 1.0).cuda().to(c.k.dtype)[:, None, None]
+    c.q[:] = torch.linspace(0.05, 0.5, c.rows * c.Hq, device="cuda").view(c.rows, c.Hq, 1).to(c.q.dtype)
+    value = (1.0 + torch.arange(D, device="cuda") / 128.0).to(c.v.dtype)
+    c.view(c.v)[:] = torch.where(torch.isinf(c.view(c.v)), c.view(c.v), value)
+    c.check(f"{lens} {new} {dt} {opts}")
+    assert torch.equal(c.out[:c.rows], value.expand(c.rows, c.Hq, D))
