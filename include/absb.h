@@ -489,7 +489,8 @@ ABSB_API int absb_rotate_store(const absb_layer* layer, const absb_rope* rope, i
 /* What a row sees and how a score is changed.  Row at position i of request b sees key j if
  *   j < L_b,  j <= i or j < prefix_lens[b],  i - j < window (if set),  and  j >= doc_start[row] (if set).
  * score = sm_scale * q.k;  then softcap * tanh(score / softcap) (if set);  then - slopes[head] * |i - j| (if
- * set).  All zero and NULL: causal attention.  A row that sees nothing yields out = 0, lse = -inf. */
+ * set).  All zero and NULL: causal attention.  A row that sees nothing yields out = 0, lse = -inf.  The cap is off by at most
+ * 3 * 2^-23 softcap for caps up to 64, by 2^-19 of the capped score for wider ones. */
 typedef struct absb_score_opts {
   float softcap;              /* 0 = none, else 1e-30 to 1e30                                    */
   int32_t window;             /* 0 = none, else >= 1: tokens a row sees up to and including itself      */

@@ -139,16 +139,17 @@ struct State {
 };
 
 // Scores q.k in log2 units: the cap, then the distance bias (`away`: from the row to the key).  CAP_WIDE: a cap so far above
-// ordinary scores that small ones need another form.
+// ordinary scores that small ones need another form, whose error is in proportion to the score.
 enum : int { CAP_NONE = 0, CAP_PLAIN = 1, CAP_WIDE = 2 };
 template <int CAP, bool BIAS>
 __device__ __forceinline__ float score_of(const AttendParams& p, float s, float slope_log2, float away) {
   float x = s;
   if (CAP) {
-    // cap tanh(y) = cap - 2 cap / (e^2y + 1), off by 2^-23 cap at most ...
+    // cap tanh(y) = cap - 2 cap / (e^2y + 1).  The exponential and the reciprocal are good to 2^-23 of themselves, the sum to 2^-24:
+    // off by 2 * 2^-23 cap around y = 0, by 3 * 2^-23 cap at most (where tanh is near -1) ...
     const float u = s * p.cap_in;  // 2 y log2(e)
     x = __builtin_fmaf(-2.0f * p.cap_log2, __builtin_amdgcn_rcpf(exp2_fast(u) + 1.0f), p.cap_log2);
-    if (CAP == CAP_WIDE) {  // ... or, for small y, the series
+    if (CAP == CAP_WIDE) {  // ... that is by 10 * 2^-23 of the result where |y| >= 1/4; for smaller ones, the series
       const float y = u * (0.5f * LN2), z = y * y;
       const float series = y * (1.0f + z * (-1.0f / 3 + z * (2.0f / 15 + z * (-17.0f / 315 + z * (62.0f / 2835)))));
       x = __builtin_fabsf(y) < 0.25f ? series * p.cap_log2 : x;
@@ -880,7 +881,7 @@ template <int DT>
 static void launch_typed(const AttendParams& p, const AttendPlan& plan, float softcap, hipStream_t stream) {
   if (softcap == 0.0f)
     launch_capped<DT, CAP_NONE>(p, plan.rows, stream);
-  else if (softcap <= 256.0f)  // (its rounding error, in units of a score: 256 / 2^23)
+  else if (softcap <= 64.0f)  // (small scores are then off by 64 * 2^-22 = 2^-16 at most)
     launch_capped<DT, CAP_PLAIN>(p, plan.rows, stream);
   else
     launch_capped<DT, CAP_WIDE>(p, plan.rows, stream);

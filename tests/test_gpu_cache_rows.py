@@ -817,3 +817,27 @@ def test_attend_outputs_stay_weighted_means(dt, lens, new, shared, opts):
     c.view(c.v)[:] = torch.where(torch.isinf(c.view(c.v)), c.view(c.v), value)
     c.check(f"{lens} {new} {dt} {opts}")
     assert torch.equal(c.out[:c.rows], value.expand(c.rows, c.Hq, D))
+
+
+@pytest.mark.parametrize("cap", [0.5, 30.0, 50.0, 64.0, 64.5, 100.0, 256.0, 257.0, 2000.0, 1e6])
+@pytest.mark.parametrize("lens,new", [([300], [300]), ([3] * 50, [3] * 50)])
+def test_attend_caps_are_as_exact_as_they_say(cap, lens, new):
+    """Every row sees itself alone, and its score is one product, so that lse is the capped score.  Beside the stated error of the cap
+    (3 * 2^-23 cap up to 64, else 2^-19 |x|), the angle's two factors and its product, the result's factor and product
+    are off by 2^-24 each: 2^-21 |x|, and 2^-149 where nothing is left to be relative to."""
+    torch = _torch()
+    c = Call(lens, new, 8, 2, 16, "f16", softcap=cap, window=1, seed=3)
+    c.k[..., 1:] = torch.where(torch.isnan(c.k[..., 1:]), c.k[..., 1:], 0.0)
+    # arguments of tanh: 0.25 either way, most of them, up to a few; with sqrt(128) for the scale
+    y = torch.linspace(-1.2, 1.2, c.rows * c.Hq, device="cuda", dtype=torch.float64)
+    y = torch.where(torch.arange(len(y), device="cuda") % 3 == 0, y * 3, y * 0.4).view(c.rows, c.Hq)
+    most = min(60000.0, 40 * cap)
+    c.q[:, :, 0] = (y / 4 * most).to(c.q.dtype)
+    c.k[..., 0] = torch.where(torch.isnan(c.k[..., 0]), c.k[..., 0], cap * math.sqrt(D) * 4 / most).to(c.k.dtype)
+    c.run()
+    torch.cuda.synchronize()
+    x = c.plain()[1]
+    assert (x.abs() > 0.9 * cap).any() and (x.abs() < 0.1 * cap).any()
+    far = (c.lse[:c.rows].double() - x).abs() - ((3 * 2.0 ** -23 * cap if cap <= 64 else 2.0 ** -19 * x.abs()) + 2.0 ** -21 * x.abs() + 2.0 ** -149)
+    _say(f"    cap {cap} {new[:2]}: max|lse - plain| {float((c.lse[:c.rows].double() - x).abs().max()):.2e}, of it beyond {float(far.max()):.2e}")
+    assert float(far.max()) <= 0
