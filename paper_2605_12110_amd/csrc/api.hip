@@ -352,9 +352,11 @@ static AttendPhase cut_phase(const PhaseSums& s, int log2_tile, int64_t splits, 
 //   32-row tiles are bound by memory, 6.0 TB/s, or, if they are few, by what one work-group can ask for: 0.0093 us a key.
 //   The two share a launch well.  Partial results are written and read, against the launch's own bytes; the merge is a launch of
 //   its own.
-// `whole`: tiles of the second phase that are not cut (then they are equal, and the only phase's).
-static double attend_us(const PhaseSums (&s)[2], const AttendPhase (&ph)[2], double pairs, int Hkv, int64_t whole) {
-  constexpr double CUS = 256, PLACES = 2 * CUS, KEY_ALONE = 0.018, KEY_PAIRED = 0.036, KEY_NARROW = 0.0093, BYTES_US = 6.0e6, START = 8, MERGE = 5;
+// `whole`: tiles of the second phase that are not cut (then they are equal, and the only phase's).  `idle`: work-groups that find no
+// rows, 1.4 to 1.7 ns each (a token behind 128 K in 64 stretches: 87 us alone, 132 behind 63 idle requests, 285 behind 255, 939 behind 999),
+// half of it beside others' keys: priced so, 83, 110 and 181 us there, and 23 behind 16 K and 63 idle ones, 23 before.
+static double attend_us(const PhaseSums (&s)[2], const AttendPhase (&ph)[2], double pairs, int Hkv, int64_t whole, double idle) {
+  constexpr double CUS = 256, PLACES = 2 * CUS, KEY_ALONE = 0.018, KEY_PAIRED = 0.036, KEY_NARROW = 0.0093, BYTES_US = 6.0e6, START = 8, MERGE = 5, IDLE = 0.0007;
   auto key_us = [&](double n) { return KEY_ALONE + (KEY_PAIRED - KEY_ALONE) * std::min(1.0, n / PLACES); };
   auto rounds = [&](double n) {  // us a key; behind a full round compute units get a second work-group only when all have one
     const double full = std::floor(n / PLACES), rest = n - full * PLACES;
@@ -388,11 +390,11 @@ static double attend_us(const PhaseSums (&s)[2], const AttendPhase (&ph)[2], dou
   }
   const double narrow = std::max(alone, bytes / BYTES_US * uneven + behind_narrow);
   const double merge = parts > 1 ? MERGE + parts / 16 + (wide > 0 ? 4 : 2) * pairs * parts * (ABSB_HEAD_DIM + 3) * 4 / BYTES_US : 0.0;
-  return START + std::max(wide, narrow) + (alone > 0 ? 0.35 * std::min(wide, narrow) : 0.0) + 2 * units / PLACES + merge;
+  return START + std::max(wide, narrow) + (alone > 0 ? 0.35 * std::min(wide, narrow) : 0.0) + 2 * units / PLACES + IDLE * idle + merge;
 }
 
-// Work-groups that a tail of tiles is cut into, at most: 68 MB of partial results.
-constexpr int TAIL_WGS = 1024;
+// Work-groups that a tail of tiles is cut into, at most: 68 MB of partial results.  Work-groups that merge a tile's parts.
+constexpr int TAIL_WGS = 1024, MERGE_WGS = 32;
 
 static int plan_attend(const absb_layer* layer, const absb_batch* batch, const absb_rows* rows, const absb_shared_prefix* shared,
                        const absb_score_opts* opts, bool any_options, AttendPlan* plan) {
@@ -468,6 +470,20 @@ static int plan_attend(const absb_layer* layer, const absb_batch* batch, const a
   int64_t slots[2];
   for (int i = 0; i < 2; ++i) slots[i] = owners[i] <= DENSE_OWNERS ? sums[i].tiles : (((int64_t)off[Bt] * G) >> tile[i]) + owners[i];
   auto work_groups = [&](const AttendPhase (&ph)[2]) { return (ph[0].slots * ph[0].splits + ph[1].whole + (ph[1].slots - ph[1].whole) * ph[1].splits) * Hkv; };
+  // All wide tiles but the last `whole` of a phase of own keys: their slots, empty ones included, and the rows of q up to their last.
+  struct Tail {
+    int64_t cut_slots, cut_rows;
+  };
+  auto tail_of = [&](int64_t whole) {
+    Tail t = {slots[1], p.rows};
+    for (int b = Bt - 1; whole > 0; --b) {
+      const int64_t n = (off[b + 1] - off[b]) * (int64_t)G, tiles = n ? ((n - 1) >> 7) + 1 : 0, cut = std::max<int64_t>(tiles - whole, 0);
+      whole -= tiles - cut;
+      t.cut_slots = Bt <= DENSE_OWNERS ? t.cut_slots - (tiles - cut) : (((int64_t)off[b] * G) >> 7) + b + cut;
+      t.cut_rows = off[b] + ceil_div(cut * 128, G);
+    }
+    return t;
+  };
   auto choose = [&](const PhaseSums (&s)[2], int most_splits) {
     double whole[2], best = 0;
     for (int i = 0; i < 2; ++i) whole[i] = s[i].max_keys * (tile[i] == 7 ? 2.0 : 1.0);
@@ -476,26 +492,35 @@ static int plan_attend(const absb_layer* layer, const absb_batch* batch, const a
       const double stretch = std::max(whole[0], whole[1]) / cuts;
       for (int i = 0; i < 2; ++i) ph[i] = cut_phase(s[i], tile[i], (int64_t)std::ceil(whole[i] / stretch - 1e-6), owners[i], slots[i]);
       if (ph[1].splits > most_splits || (cuts > 1 && work_groups(ph) > MAX_WGS)) break;
-      const double us = attend_us(s, ph, (double)p.rows * layer->num_q_heads, Hkv, 0);
+      double idle = 0;
+      for (int i = 0; i < 2; ++i) idle += (double)(ph[i].slots - (ph[i].owners ? s[i].tiles : 0)) * Hkv * ph[i].splits;
+      const double us = attend_us(s, ph, (double)p.rows * layer->num_q_heads, Hkv, 0, idle);
       // (as good as level: fewer parts, unless they are those of narrow tiles, which are small)
-      if (cuts > 1 && us >= (tile[0] == 7 || tile[1] == 7 ? 0.98 : 0.998) * best) continue;
+      if (cuts > 1 && us >= ((ph[0].owners && tile[0] == 7) || tile[1] == 7 ? 0.98 : 0.998) * best) continue;
       best = us;
       p.shared = ph[0];
       p.own = ph[1];
+      p.cut_rows = p.rows;
     }
     // (About) equal wide tiles that fill the chip and a bit: those that are left over are cut, into at most TAIL_WGS work-groups (560
     // tiles of 4096 capped scores: 250 us with none cut or all, 198; 640 of them without a cap 207 -> 198, 768 best as they are).
+    // Idle requests ahead of them have slots that are cut and merged as well.
     const int64_t places = 512 / Hkv, full = s[1].tiles / std::max<int64_t>(places, 1) * places, rest = s[1].tiles - full;
-    if (shared || tile[1] != 7 || !full || !rest || (rest + Bt) * Hkv * 32 > MAX_WGS || 20 * s[1].keys < 17.0 * s[1].tiles * s[1].max_keys) return;
+    if (shared || tile[1] != 7 || !full || !rest || 20 * s[1].keys < 17.0 * s[1].tiles * s[1].max_keys) return;
+    const Tail tail = tail_of(full);
     AttendPhase ph[2] = {};
+    if (tail.cut_slots * Hkv * MERGE_WGS > MAX_WGS) return;
     for (int cuts = 2; cuts <= 64 && rest * Hkv * cuts <= TAIL_WGS; ++cuts) {
       ph[1] = cut_phase(s[1], 7, cuts, owners[1], slots[1]);
+      ph[1].whole = slots[1] - tail.cut_slots;
+      if (work_groups(ph) > MAX_WGS) break;
       if (ph[1].splits != cuts) continue;
-      const double us = attend_us(s, ph, (double)p.rows * layer->num_q_heads, Hkv, full);
+      const double idle = (double)(ph[1].whole - full + (tail.cut_slots - rest) * (cuts + MERGE_WGS)) * Hkv;
+      const double us = attend_us(s, ph, (double)p.rows * layer->num_q_heads, Hkv, full, idle);
       if (us >= 0.98 * best) continue;
       best = us;
       p.own = ph[1];
-      p.own.whole = full;
+      p.cut_rows = tail.cut_rows;
     }
   };
   int64_t parts_any = 0, tail_any = 0;  // the most that any options make: of all rows; partial results of a tail
@@ -513,17 +538,6 @@ static int plan_attend(const absb_layer* layer, const absb_batch* batch, const a
     }
   }
   p.parts = p.shared.splits + p.own.splits;
-  p.cut_rows = p.rows;
-  if (p.own.whole) {  // tiles to slots: the last owners' are whole
-    int64_t left = p.own.whole, slot = slots[1];
-    for (int b = Bt - 1; left > 0; --b) {
-      const int64_t n = (off[b + 1] - off[b]) * (int64_t)G, tiles = n ? ((n - 1) >> 7) + 1 : 0, cut = std::max<int64_t>(tiles - left, 0);
-      left -= tiles - cut;
-      slot = Bt <= DENSE_OWNERS ? slot - (tiles - cut) : (((int64_t)off[b] * G) >> 7) + b + cut;
-      p.cut_rows = off[b] + ceil_div(cut * 128, G);
-    }
-    p.own.whole = slots[1] - slot;
-  }
   if (work_groups({p.shared, p.own}) > MAX_WGS) return ABSB_ERR_BAD_SHAPE;
   // Owners of one tile have their rows read once; what the last-level cache could not keep for the next call anyway passes it by.
   // Narrow: one token behind 128 K 101 -> 88 us, 64 behind 2 K 95 -> 84, 64 behind 1 K, 134 MB, 50.3 -> 44.7.  Wide: 12 behind 128 K

@@ -248,3 +248,28 @@ def test_workspace_sizes(lens, new):
         assert absb.absb_attend_workspace(_layer(), _batch(lens), _rows(new), None, opts) <= size
     with pytest.raises(absb.AbsbError):
         absb.absb_attend_workspace(_layer(), _batch(lens), _rows(new), None, absb.ScoreOpts(window=-1))
+
+
+# ------------------------------------------------------------------ requests without rows
+def _idle(B, at, new, L, shared=None, opts=absb.ScoreOpts()):
+    lens, n = np.zeros(B, np.int32), np.zeros(B, np.int32)
+    lens[at], n[at] = L, new
+    return absb.absb_attend_workspace(_layer(), _batch(lens), _rows(n), shared, opts)
+
+
+def test_a_chunk_behind_many_idle_requests_is_planned():
+    """65 tiles of 128 rows, 64 of which fill the chip: whichever request of many brings them.  (2080 rows of 32 heads, 524 bytes a
+    partial result: no more of them than a cut in 64 of one tile, or in two of all.)"""
+    one = _idle(1, 0, 2080, 2080 + (1 << 17))
+    assert 0 < one <= 1024 * 128 * 524 + 512
+    for B in (40, 64, 1000, 60000, 65535):
+        for at in (0, B // 2, B - 1):
+            assert _idle(B, at, 2080, 2080 + (1 << 17)) <= 2 * 2080 * 32 * 524 + 512, (B, at)
+    assert _idle(63, 62, 2080, 2080 + (1 << 17)) == one
+
+
+def test_idle_requests_do_not_multiply_the_cuts():
+    """One token behind 128 Ki, alone: 64 stretches, 8 x 64 work-groups.  Idle requests' slots are launched as often as the tile is cut."""
+    parts = [_idle(B, B - 1, 1, 1 << 17) // (32 * 524) for B in (1, 63, 64, 256, 1000, 60000)]
+    assert parts[0] == parts[1] == 64
+    assert all(a >= b for a, b in zip(parts, parts[1:])) and parts[2] >= 8 and 999 * 8 * parts[4] < 100000 and 60000 * 8 * parts[5] < 1 << 21

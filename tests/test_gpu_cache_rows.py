@@ -841,3 +841,22 @@ def test_attend_caps_are_as_exact_as_they_say(cap, lens, new):
     far = (c.lse[:c.rows].double() - x).abs() - ((3 * 2.0 ** -23 * cap if cap <= 64 else 2.0 ** -19 * x.abs()) + 2.0 ** -21 * x.abs() + 2.0 ** -149)
     _say(f"    cap {cap} {new[:2]}: max|lse - plain| {float((c.lse[:c.rows].double() - x).abs().max()):.2e}, of it beyond {float(far.max()):.2e}")
     assert float(far.max()) <= 0
+
+
+@pytest.mark.parametrize("B,at", [(63, (0, 30, 62)), (64, (0, 31, 63)), (90, (89,)), (300, (0,)), (300, (7, 150, 151)), (400, (399,))])
+@pytest.mark.parametrize("opts", [dict(), dict(window=20000)])
+def test_attend_of_a_tail_among_idle_requests(B, at, opts):
+    """Equal tiles that fill the chip and a bit, brought by a few of many requests: which tiles are cut, and whose parts are merged,
+    goes by slots, of which idle requests have one each."""
+    lens, new = np.zeros(B, np.int64), np.zeros(B, np.int64)
+    for i, b in enumerate(at):
+        new[b] = 1050 // len(at) + i
+        lens[b] = 30000 - 7 * i
+    for dt in ("f16", "bf16"):
+        c = Call(lens, new, 64, 8, 16, dt, seed=B, **opts)                   # 66 tiles a head, places for 64
+        # (partial results of some rows only)
+        assert 0 < _absb().absb_attend_workspace(c.layer, c.batch, c.r, None, c.opts) < c.rows * 64 * 524
+        n = c.ws.numel() - 256
+        c.ws, guard = c.ws[:n], c.ws[n:]
+        c.check(f"{B} requests, rows of {at} {dt} {opts}")
+        assert (guard == 0xA5).all()
