@@ -882,7 +882,7 @@ int absb_rotate_store(const absb_layer* layer, const absb_rope* rope, int32_t n_
   if (rc != ABSB_OK) return rc;
   rc = check_rope(rope);
   if (rc != ABSB_OK) return rc;
-  if (n_rows < 0 || n_rows >= 1 << 26) return ABSB_ERR_BAD_SHAPE;  // (four rows a work-group)
+  if (n_rows < 0 || n_rows > 4 * MAX_WGS) return ABSB_ERR_BAD_SHAPE;  // (four rows a work-group)
   if (n_rows == 0) return ABSB_OK;
   if (!row_pos || !freq || !q != !q_out || !k != !v || (!q && !k)) return ABSB_ERR_NULL;
   if (k && (!row_slot || !k_cache || !v_cache)) return ABSB_ERR_NULL;

@@ -273,3 +273,10 @@ def test_idle_requests_do_not_multiply_the_cuts():
     parts = [_idle(B, B - 1, 1, 1 << 17) // (32 * 524) for B in (1, 63, 64, 256, 1000, 60000)]
     assert parts[0] == parts[1] == 64
     assert all(a >= b for a, b in zip(parts, parts[1:])) and parts[2] >= 8 and 999 * 8 * parts[4] < 100000 and 60000 * 8 * parts[5] < 1 << 21
+
+
+# ------------------------------------------------------------------ limits and what the binding looks at
+@pytest.mark.parametrize("n", [(1 << 26) - 3, (1 << 26) - 1])
+def test_rotate_store_of_more_rows_than_a_launch_has_threads_for(n):
+    """Four rows a work-group of 256 threads: from 2^26 - 3 rows on, 2^32 threads."""
+    _refused(absb.ERR_BAD_SHAPE, absb.absb_rotate_store, **_rot(n=n))
