@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import sys
 import threading
 from dataclasses import dataclass
 from typing import Optional, Sequence
@@ -145,9 +146,48 @@ def _check(status: int, where: str) -> None:
 
 
 def _ptr(t) -> Optional[int]:
-    if t is None or isinstance(t, int):
+    if t is None:
+        return None
+    try:
+        return t.data_ptr()
+    except AttributeError:
+        if isinstance(t, int):
+            return t
+        raise
+
+
+def _long(t, nbytes: int, where: str) -> Optional[int]:
+    """Address of a tensor of so many bytes at least.  None and addresses pass.  (One look at it, in front of calls of 3 us.)"""
+    try:
+        if t.nbytes >= nbytes:
+            return t.data_ptr()
+    except AttributeError:
+        return _ptr(t)
+    raise AbsbError(ERR_BAD_SHAPE, where)
+
+
+def _dense(t, nbytes: int, where: str) -> Optional[int]:
+    """The same, of values side by side."""
+    if t is None or t.__class__ is int:
         return t
-    return t.data_ptr()
+    if not t.is_contiguous():
+        raise AbsbError(ERR_BAD_SHAPE, where)
+    return _long(t, nbytes, where)
+
+
+_value_types = {}        # a layer's dtype -> torch's
+
+
+def _value_type(dtype: int):
+    """torch's type of a layer's values; None where torch is not in use, or knows none."""
+    if not _value_types and "torch" in sys.modules:
+        torch = sys.modules["torch"]
+        _value_types.update({F16: torch.float16, BF16: torch.bfloat16})
+    return _value_types.get(dtype)
+
+
+def _other(t, kind) -> bool:
+    return kind is not None and getattr(t, "dtype", kind) is not kind
 
 
 _raw_stream = None
@@ -345,7 +385,7 @@ class Rows(_Record):
 
     def _make(self):
         a, at = _i32_host(self.row_off_host)
-        rec = _Rows(at, _ptr(self.row_off))
+        rec = _Rows(at, _dense(self.row_off, 0 if a is None else 4 * len(a), "absb_rows"))
         rec._arrays = (a,)
         return rec
 
@@ -358,7 +398,8 @@ class PageRing(_Record):
     cursors: object
 
     def _make(self):
-        return _Ring(_ptr(self.pages), self.pages.numel(), _ptr(self.cursors), _ptr(self.cursors))
+        n, cursors = self.pages.numel(), _dense(self.cursors, 32, "absb_page_ring")
+        return _Ring(_dense(self.pages, 4 * n, "absb_page_ring"), n, cursors, cursors)
 
 
 @dataclass
@@ -392,6 +433,12 @@ class ScoreOpts(_Record):
     def _make(self):
         return _ScoreOpts(float(self.softcap), int(self.window), _ptr(self.slopes), _ptr(self.prefix_lens), _ptr(self.doc_start))
 
+    def fits(self, heads: int, requests: int, rows: int, where: str) -> None:
+        """Refuses tensors that are shorter than what the call reads."""
+        _dense(self.slopes, 4 * heads, where)
+        _dense(self.prefix_lens, 4 * requests, where)
+        _dense(self.doc_start, 4 * rows, where)
+
 
 @dataclass
 class SharedPrefix(_Record):
@@ -405,7 +452,10 @@ class SharedPrefix(_Record):
     def _make(self):
         a, a_at = _i32_host(self.first_host)
         n, n_at = _i32_host(self.len_host)
-        rec = _Shared(len(n), a_at, n_at, _ptr(self.first), _ptr(self.length))
+        if len(a) != len(n) + 1:
+            raise AbsbError(ERR_BAD_SHAPE, "absb_shared_prefix")
+        rec = _Shared(len(n), a_at, n_at, _dense(self.first, 4 * len(a), "absb_shared_prefix"),
+                      _dense(self.length, 4 * len(n), "absb_shared_prefix"))
         rec._arrays = (a, n)
         return rec
 
@@ -535,21 +585,29 @@ def absb_assign_block_sizes(recall: np.ndarray, candidates: Sequence[int], tau: 
     return out, mean
 
 
+def _tables_fit(t, requests: int, pt_stride: int) -> bool:
+    """Whether page tables that are not the batch's own have as many rows, as far apart (a view of wider ones, say)."""
+    return t is None or t.__class__ is int or t.nbytes >= 4 * requests * pt_stride or (
+        t.shape[0] >= requests and t.stride()[0] >= pt_stride)
+
+
 def absb_map_rows(layer: Layer, batch: Batch, lens_before, page_table, row_off, row_pos, row_slot, ring: PageRing = None,
                   cursors_out=None, stream=None) -> None:
     """`row_pos` and `row_slot` are as long as the most rows that the step may have; `cursors_out` None: in place."""
-    cl, cb = layer.c(), batch.c()
+    cl, cb, where, n = layer.c(), batch.c(), "absb_map_rows", row_pos.numel()
+    requests = cb.batch
     rec = None
     if ring is not None:
         rec = ring.c()
         if cursors_out is not None:
             rec = _Ring.from_buffer_copy(rec)
-            rec.cursors_out = _ptr(cursors_out)
+            rec.cursors_out = _long(cursors_out, 32, where)
         rec = C.byref(rec)
-    if row_pos.numel() != row_slot.numel():
-        raise AbsbError(ERR_BAD_SHAPE, "absb_map_rows")
-    _check(load().absb_map_rows(C.byref(cl), C.byref(cb), _ptr(lens_before), _ptr(page_table), rec, row_pos.numel(), _ptr(row_off),
-                                _ptr(row_pos), _ptr(row_slot), _stream(stream)), "absb_map_rows")
+    if row_slot.numel() != n or (page_table is not batch.page_table and not _tables_fit(page_table, requests, cb.pt_stride)):
+        raise AbsbError(ERR_BAD_SHAPE, where)
+    _check((_lib or load()).absb_map_rows(C.byref(cl), C.byref(cb), _long(lens_before, 4 * requests, where), _ptr(page_table), rec,
+                                          n, _long(row_off, 4 * requests + 4, where), _long(row_pos, 4 * n, where),
+                                          _long(row_slot, 8 * n, where), _stream(stream)), where)
 
 
 def absb_rope_frequencies(rope: Rope) -> np.ndarray:
@@ -559,10 +617,10 @@ def absb_rope_frequencies(rope: Rope) -> np.ndarray:
     return out[:int(rope.rot_dim) // 2].copy()
 
 
-def _row_stride(t, rows: int, heads: int, where: str) -> int:
-    """Of a [rows][heads][128] tensor whose heads and channels are dense."""
-    shape, stride = t.shape, t.stride()
-    if tuple(shape) != (rows, heads, 128) or stride[1] != 128 or stride[2] != 1:
+def _row_stride(t, kind, rows: int, heads: int, where: str) -> int:
+    """Of a [rows][heads][128] tensor of the layer's type whose heads and channels are dense."""
+    stride = t.stride()
+    if t.shape != (rows, heads, 128) or stride[1] != 128 or stride[2] != 1 or _other(t, kind):
         raise AbsbError(ERR_BAD_SHAPE, where)
     return stride[0] if rows > 1 else heads * 128
 
@@ -571,37 +629,54 @@ def absb_rotate_store(layer: Layer, rope: Rope, row_pos, row_slot, freq, q=None,
                       v_cache=None, stream=None) -> None:
     """q, k, v: [rows][heads][128], rows any multiple of 8 elements apart (views of one projection's output, say)."""
     cl, where, n = layer.c(), "absb_rotate_store", row_pos.numel()
-    qs = 0 if q is None else _row_stride(q, n, cl.num_q_heads, where)
-    ks = 0 if k is None else _row_stride(k, n, cl.num_kv_heads, where)
-    vs = 0 if v is None else _row_stride(v, n, cl.num_kv_heads, where)
+    kind = _value_type(cl.dtype)
+    qs = 0 if q is None else _row_stride(q, kind, n, cl.num_q_heads, where)
+    ks = 0 if k is None else _row_stride(k, kind, n, cl.num_kv_heads, where)
+    vs = 0 if v is None else _row_stride(v, kind, n, cl.num_kv_heads, where)
     if row_slot is not None and row_slot.numel() != n:
         raise AbsbError(ERR_BAD_SHAPE, where)
-    if q_out is not None and (not q_out.is_contiguous() or q_out.numel() != n * cl.num_q_heads * 128):
+    if q_out is not None and (not q_out.is_contiguous() or q_out.numel() != n * cl.num_q_heads * 128 or _other(q_out, kind)):
         raise AbsbError(ERR_BAD_SHAPE, where)
-    _check(load().absb_rotate_store(C.byref(cl), _rec(rope), n, _ptr(row_pos), _ptr(row_slot), _ptr(freq), _ptr(q), qs, _ptr(q_out),
-                                    _ptr(k), ks, _ptr(v), vs, _ptr(k_cache), _ptr(v_cache), _stream(stream)), where)
+    _check((_lib or load()).absb_rotate_store(
+        C.byref(cl), _rec(rope), n, _long(row_pos, 4 * n, where), _long(row_slot, 8 * n, where), _long(freq, 4 * int(rope.rot_dim), where),
+        _ptr(q), qs, _ptr(q_out), _ptr(k), ks, _ptr(v), vs, _ptr(k_cache), _ptr(v_cache), _stream(stream)), where)
 
 
 def absb_attend_workspace(layer: Layer, batch: Batch, rows: Rows, shared: SharedPrefix = None, opts: ScoreOpts = None) -> int:
     """Bytes; without `opts`: enough for any options."""
     cl, cb = layer.c(), batch.c()
+    _rows_of(rows, cb, "absb_attend_workspace")
     n = C.c_size_t(0)
     _check(load().absb_attend_workspace(C.byref(cl), C.byref(cb), _rec(rows), _rec(shared), _rec(opts), C.byref(n)), "absb_attend_workspace")
     return int(n.value)
 
 
-def _dense(where: str, heads: int, rows: Rows, *tensors) -> None:
-    """Queries and outputs: dense, and as many rows as the step has."""
-    for t in tensors:
+def _rows_of(rows: Rows, batch: _Batch, where: str) -> int:
+    """How many rows a step has, of as many requests as the batch."""
+    off = rows.row_off_host
+    if off is None:
+        return 0
+    if len(off) != batch.batch + 1:
+        raise AbsbError(ERR_BAD_SHAPE, where)
+    return int(off[-1])
+
+
+def _step(where: str, layer: _Layer, batch: _Batch, rows: Rows, q, out, lse, opts: Optional[ScoreOpts]) -> None:
+    """Refuses queries and outputs of another type, and what is not dense or shorter than the step: these, log-sums, options."""
+    n, heads, kind = _rows_of(rows, batch, where), layer.num_q_heads, _value_type(layer.dtype)
+    for t in (q, out):
         if t is not None and t.__class__ is not int:
-            if not t.is_contiguous() or (rows.row_off_host is not None and t.numel() < int(rows.row_off_host[-1]) * heads * 128):
+            if not t.is_contiguous() or t.numel() < n * heads * 128 or _other(t, kind):
                 raise AbsbError(ERR_BAD_SHAPE, where)
+    _dense(lse, 4 * n * heads, where)
+    if opts is not None and (opts.slopes is not None or opts.prefix_lens is not None or opts.doc_start is not None):
+        opts.fits(heads, batch.batch, n, where)
 
 
 def absb_attend_rows(layer: Layer, batch: Batch, rows: Rows, q, k_cache, v_cache, out, lse=None, opts: ScoreOpts = None,
                      workspace=None, stream=None) -> None:
     cl, cb = layer.c(), batch.c()
-    _dense("absb_attend_rows", cl.num_q_heads, rows, q, out)
+    _step("absb_attend_rows", cl, cb, rows, q, out, lse, opts)
     _check(load().absb_attend_rows(C.byref(cl), C.byref(cb), _rec(rows), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(out), _ptr(lse),
                                    _rec(opts), _ptr(workspace), _nbytes(workspace), _stream(stream)), "absb_attend_rows")
 
@@ -609,7 +684,7 @@ def absb_attend_rows(layer: Layer, batch: Batch, rows: Rows, q, k_cache, v_cache
 def absb_attend_shared(layer: Layer, batch: Batch, rows: Rows, shared: SharedPrefix, q, k_cache, v_cache, out, lse=None,
                        opts: ScoreOpts = None, workspace=None, stream=None) -> None:
     cl, cb = layer.c(), batch.c()
-    _dense("absb_attend_shared", cl.num_q_heads, rows, q, out)
+    _step("absb_attend_shared", cl, cb, rows, q, out, lse, opts)
     _check(load().absb_attend_shared(C.byref(cl), C.byref(cb), _rec(rows), _rec(shared), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(out),
                                      _ptr(lse), _rec(opts), _ptr(workspace), _nbytes(workspace), _stream(stream)), "absb_attend_shared")
 

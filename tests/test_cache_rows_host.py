@@ -280,3 +280,55 @@ def test_idle_requests_do_not_multiply_the_cuts():
 def test_rotate_store_of_more_rows_than_a_launch_has_threads_for(n):
     """Four rows a work-group of 256 threads: from 2^26 - 3 rows on, 2^32 threads."""
     _refused(absb.ERR_BAD_SHAPE, absb.absb_rotate_store, **_rot(n=n))
+
+
+def _zeros(*shape, **kw):
+    import torch
+    kw.setdefault("dtype", torch.float32)
+    return torch.zeros(*shape, **kw)
+
+
+def _torch_types():
+    import torch
+    return torch.float16, torch.bfloat16, torch.int32, torch.int64, torch.float64
+
+
+def test_attend_refuses_tensors_shorter_than_the_step():
+    """3 rows of 32 heads of two requests: what a call would write or read behind a tensor's end, or beside its rows."""
+    f16, bf16, i32, i64, f64 = _torch_types()
+    layer, batch, rows = _layer(), _batch((100, 200)), _rows((1, 2))
+    short = [dict(lse=_zeros(3, 31)), dict(lse=_zeros(2, 32)), dict(lse=_zeros(3, 64)[:, :32]), dict(lse=_zeros(3, 32, dtype=f16)),
+             dict(q=_zeros(3, 32, D)), dict(q=_zeros(3, 32, D, dtype=bf16)), dict(out=_zeros(3, 32, D)), dict(out=_zeros(2, 32, D, dtype=f16)),
+             dict(opts=absb.ScoreOpts(slopes=_zeros(31))), dict(opts=absb.ScoreOpts(slopes=_zeros(64)[::2])),
+             dict(opts=absb.ScoreOpts(prefix_lens=_zeros(1, dtype=i32))), dict(opts=absb.ScoreOpts(doc_start=_zeros(2, dtype=i32))),
+             dict(rows=absb.Rows([0, 1, 3], _zeros(2, dtype=i32))), dict(rows=absb.Rows([0, 3], AT)), dict(rows=absb.Rows([0, 1, 2, 3], AT))]
+    for kw in short:
+        d = dict(rows=rows, q=AT, out=AT, lse=None, opts=None)
+        d.update(kw)
+        _refused(absb.ERR_BAD_SHAPE, absb.absb_attend_rows, layer, batch, d["rows"], d["q"], AT, AT, d["out"], d["lse"], d["opts"], BIG_WS)
+        _refused(absb.ERR_BAD_SHAPE, absb.absb_attend_shared, layer, batch, d["rows"], absb.SharedPrefix([0, 2], [0], AT, AT), d["q"], AT, AT,
+                 d["out"], d["lse"], d["opts"], BIG_WS)
+    for r in (absb.Rows([0, 3], AT), absb.Rows([0, 1, 2, 3], AT)):
+        with pytest.raises(absb.AbsbError) as e:
+            absb.absb_attend_workspace(layer, batch, r)
+        assert e.value.status == absb.ERR_BAD_SHAPE
+    for shared in (absb.SharedPrefix([0, 2], [0, 0], AT, AT), absb.SharedPrefix([0, 2], [0], _zeros(1, dtype=i32), AT),
+                   absb.SharedPrefix([0, 2], [0], AT, _zeros(0, dtype=i32))):
+        _refused(absb.ERR_BAD_SHAPE, absb.absb_attend_shared, layer, batch, rows, shared, AT, AT, AT, AT, None, None, BIG_WS)
+
+
+def test_rotate_and_map_refuse_tensors_shorter_than_the_step():
+    f16, bf16, i32, i64, f64 = _torch_types()
+    for kw in (dict(freq=_zeros(63, dtype=f64)), dict(freq=_zeros(64)), dict(rope=absb.Rope(rot_dim=66), freq=_zeros(32, dtype=f64)),
+               dict(row_pos=_zeros(3, dtype=f16)), dict(row_slot=_zeros(3, dtype=i32)), dict(q=_zeros(3, 32, D)), dict(q=_zeros(3, 32, D, dtype=bf16)),
+               dict(q_out=_zeros(3, 32, D)), dict(k=_zeros(3, 8, D)), dict(v=_zeros(3, 8, D, dtype=bf16))):
+        _refused(absb.ERR_BAD_SHAPE, absb.absb_rotate_store, **_rot(**kw))
+    batch = _batch((5, 6), width=4)
+    ring = lambda **kw: absb.PageRing(**dict(dict(pages=_zeros(9, dtype=i32), cursors=_zeros(4, dtype=i64)), **kw))  # noqa: E731
+    for kw in (dict(before=_zeros(1, dtype=i32)), dict(off=_zeros(2, dtype=i32)), dict(table=_zeros(1, 4, dtype=i32)), dict(table=_zeros(2, 3, dtype=i32)),
+               dict(pos=_zeros(4, dtype=f16)), dict(slot=_zeros(4, dtype=i32)), dict(ring=ring(cursors=_zeros(3, dtype=i64))),
+               dict(ring=ring(cursors=_zeros(4, dtype=i32))), dict(ring=ring(pages=_zeros(9, dtype=f16)))):
+        d = dict(before=AT, table=AT, off=AT, pos=_T(4), slot=_T(4), ring=None)
+        d.update(kw)
+        _refused(absb.ERR_BAD_SHAPE, absb.absb_map_rows, _layer(), batch, *d.values())
+    _refused(absb.ERR_BAD_SHAPE, absb.absb_map_rows, *_map(batch=batch, ring=ring()), cursors_out=_zeros(3, dtype=i64))
