@@ -383,13 +383,17 @@ __device__ __forceinline__ Stretch stretch_on(const AttendParams& p, int32_t pag
 // compiler would wait for every copy in flight ahead of every read of LDS, the one of the next block included.  (It must wait
 // for none: copies_done() does, in front of the barrier behind which a block is read.  The waits: m0 wants one state ahead of the
 // copy, a scalar that came from a vector instruction five.)
+// (m0 is nobody's register, which the compiler warns of; that the copy changes it is said all the same, should it come to use it.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 template <bool STREAM>  // past the caches
 __device__ __forceinline__ void copy_to_lds(const char* base, uint32_t lane_off, uint32_t to) {
   if (STREAM)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(to), "v"(lane_off), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(to), "v"(lane_off), "s"(base) : "memory", "m0");
   else
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(lane_off), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(lane_off), "s"(base) : "memory", "m0");
 }
+#pragma clang diagnostic pop
 __device__ __forceinline__ uint32_t lds_address(const char* at) {
   typedef __attribute__((address_space(3))) const char* lds;
   return (uint32_t)(uintptr_t)(lds)(at);
