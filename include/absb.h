@@ -475,8 +475,8 @@ ABSB_API int absb_rope_frequencies(const absb_rope* rope, double* freq_host);
  *   row_pos [n_rows] i32, row_slot [n_rows] i64 : as absb_map_rows writes them.  A row whose slot is negative
  *             has its query rotated and nothing stored.  Slots that are not negative must differ: one that two rows name ends
  *             with parts of either row's key and value.
- *   freq [rot_dim/2] f64 device : radians per position, |freq| < 2^32.  Angles are exact to 2^-32 turns + position *
- *             2^-52 |freq| at any position.
+ *   freq [rot_dim/2] f64 device : radians per position, |freq| < 2^32.  Angles are off by at most 2^-25 turns + position *
+ *             2^-52 |freq| radians, sines and cosines by 1.3e-7 more.
  *   q [n_rows][Hq][d], k, v [n_rows][Hkv][d] : rows q_stride, k_stride, v_stride elements apart (multiples of 8, so that the
  *             three may lie side by side in one projection's output), 16-byte aligned.
  *   q_out [n_rows][Hq][d] : rotated queries; may be q itself when q_stride is Hq*d, and must not overlap

@@ -195,8 +195,9 @@ int launch_map_rows(const MapParams& p, hipStream_t stream) {
 //
 // Pair (x, y) of a token at position p turns by p * f:  (x cos - y sin, x sin + y cos).  The angle is taken in turns, as a
 // 64-bit fraction F = f / 2 pi mod 1, so that p * F mod 2^64 is the exact product whatever the position: in binary32 an angle
-// of a million radians is off by 0.03.  Its upper 32 bits, as a number in [-1/2, 1/2), go to the hardware's sine and cosine
-// of turns (off by at most 1.3e-7 over that range, where a 16-bit result is off by 2^-12 at best).
+// of a million radians is off by 0.03.  Its upper 32 bits, as a number in [-1/2, 1/2), go, rounded to the 24 of
+// binary32 (2^-26 turns at most), to the hardware's sine and cosine of turns (off by at most 1.3e-7 over that range, where a 16-bit
+// result is off by 2^-12 at best).
 //
 // Bound by memory: (Hq + 2 Hkv) rows of 256 bytes in and out a token (8192 tokens of 48 heads 38.5 us, 32 K 140 us, 5.2 and 5.65 TB/s;
 // 16 tokens 4.0 us, a chain of round trips).  A lane holds 16-byte pieces (of both halves of a pair's

@@ -860,3 +860,30 @@ def test_attend_of_a_tail_among_idle_requests(B, at, opts):
         c.ws, guard = c.ws[:n], c.ws[n:]
         c.check(f"{B} requests, rows of {at} {dt} {opts}")
         assert (guard == 0xA5).all()
+
+
+@pytest.mark.parametrize("rot,pairs", [(128, False), (128, True), (64, False), (22, True)])
+def test_rotate_angles_are_as_exact_as_they_say(rot, pairs):
+    """Pairs that all but cancel, 256 (sin a, cos a) in f16 at angle a: x cos a - y sin a is what the rounding of x and y leaves, so that
+    its own rounding hides little.  Angle: 2^-25 turns = 1.9e-7, and position * 2^-52 |f|; hardware sine 1.3e-7; two factors,
+    two products and a sum in binary32: 4 * 2^-24 = 2.4e-7; the oracle's own product 2^-53 position |f|."""
+    torch, absb = _torch(), _absb()
+    pos = np.concatenate([np.arange(64), 2 ** np.arange(6, 31), 2 ** np.arange(7, 32) - 1, np.random.default_rng(1).integers(0, 1 << 20, 100)])
+    pos = pos.astype(np.int32)
+    n, half = len(pos), rot // 2
+    rope = absb.Rope(rot_dim=rot, layout=absb.ROPE_PAIRS if pairs else absb.ROPE_HALVES, base=10000.0)
+    freq = absb.absb_rope_frequencies(rope)
+    i0, i1 = (np.arange(0, rot, 2), np.arange(1, rot, 2)) if pairs else (np.arange(half), np.arange(half, rot))
+    x = np.random.default_rng(2).standard_normal((n, 1, D))
+    angle = pos[:, None].astype(np.float64) * freq[None]
+    x[:, 0, i0], x[:, 0, i1] = 256 * np.sin(angle), 256 * np.cos(angle)
+    q = torch.from_numpy(x).half().cuda()
+    out = torch.empty_like(q)
+    absb.absb_rotate_store(_layer(1, 1), rope, torch.from_numpy(pos).cuda(), None, torch.from_numpy(freq).cuda(), q, out)
+    torch.cuda.synchronize()
+    want, size = rotate_plain(q.double().cpu().numpy(), pos, freq, rot, pairs, 1.0)
+    far = np.zeros((n, 1, D))
+    far[:, 0, i0] = far[:, 0, i1] = 1.9e-7 + 1.3e-7 + 2.4e-7 + pos[:, None] * 2.0 ** -51 * freq[None]
+    err = np.abs(out.double().cpu().numpy() - want)
+    _say(f"    rot {rot}: {float(((err - STEP['f16'] * np.abs(want) - 2.0 ** -24) / np.maximum(size, 1e-9))[:, :, i0].max()):.2e} of |x| + |y|")
+    assert (err <= far * size + STEP["f16"] * np.abs(want) + 2.0 ** -24).all()
