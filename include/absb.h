@@ -434,7 +434,11 @@ typedef struct absb_page_ring {
  * request takes or gives back, then no table, no page and no cursor changes, every row_slot is -1 and cursors_out[2] (written
  * with a ring only) says how many pages were missing.  Without a ring, rows beyond the table's width get
  * slot -1.  max_rows is at most 2^30, batch at most 65535; sums of rows and of pages must stay below 2^31.  Reads batch->batch,
- * pt_stride and seq_lens, and layer->page_size. */
+ * pt_stride and seq_lens, and layer->page_size.
+ * The ring knows no owners: a page comes back as often as requests give it back.  Requests on a shared prefix (absb_attend_shared)
+ * of S tokens therefore never have a length below S in this call: one joins with a length of S before (the caller has written the
+ * prefix's pages into the first S/P entries of its row), finishes with S after, and has S both times while its row is idle.  The prefix's
+ * own pages are taken, and given back once nobody is on it, by a call for it alone. */
 ABSB_API int absb_map_rows(const absb_layer* layer, const absb_batch* batch, const int32_t* lens_before,
                            int32_t* page_table, const absb_page_ring* ring, int32_t max_rows, int32_t* row_off,
                            int32_t* row_pos, int64_t* row_slot, void* stream);

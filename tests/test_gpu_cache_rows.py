@@ -887,3 +887,68 @@ def test_rotate_angles_are_as_exact_as_they_say(rot, pairs):
     err = np.abs(out.double().cpu().numpy() - want)
     _say(f"    rot {rot}: {float(((err - STEP['f16'] * np.abs(want) - 2.0 ** -24) / np.maximum(size, 1e-9))[:, :, i0].max()):.2e} of |x| + |y|")
     assert (err <= far * size + STEP["f16"] * np.abs(want) + 2.0 ** -24).all()
+
+
+def test_the_run_of_a_server_with_a_shared_prefix():
+    """Requests on a common prefix join, grow, finish and are replaced; their own pages go through the ring, the prefix's are taken
+    and given back by a call for the prefix alone.  Every page is with one owner at any time."""
+    torch, absb = _torch(), _absb()
+    Hq, Hkv, P, S, B, pages = 8, 2, 16, 48, 4, 24
+    g = torch.Generator(device="cuda").manual_seed(21)
+    layer = _layer(Hq, Hkv, P)
+    k, v = (torch.full((pages, Hkv, P, D), float("nan"), dtype=torch.float16, device="cuda") for _ in range(2))
+    ring = absb.PageRing(torch.randperm(pages, generator=g, device="cuda").int(), torch.tensor([0, pages, 0, 0], dtype=torch.int64, device="cuda"))
+    rope, freq = absb.Rope(), torch.zeros(64, dtype=torch.float64, device="cuda")       # (no turn: keys are stored as they are)
+    up = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")  # noqa: E731
+
+    def step(table, before, after):
+        """Rows and pages, new keys and values into the cache; what `absb_attend_shared` takes."""
+        new = [max(a - b, 0) for b, a in zip(before, after)]
+        rows = sum(new)
+        off, pos, slot = up([0] * (len(new) + 1)), up([0] * rows), torch.zeros(rows, dtype=torch.int64, device="cuda")
+        batch = absb.Batch(seq_lens_host=after, seq_lens=up(after), page_table=table)
+        absb.absb_map_rows(layer, batch, up(before), table, off, pos, slot, ring)
+        qkv = torch.randn((rows, Hq + 2 * Hkv, D), generator=g, device="cuda").half()
+        q, kn, vn = qkv.split((Hq, Hkv, Hkv), 1)
+        absb.absb_rotate_store(layer, rope, pos, slot, freq, k=kn, v=vn, k_cache=k, v_cache=v)
+        rec = absb.Rows(np.concatenate([[0], np.cumsum(new)]).astype(np.int32), off)
+        assert off.tolist() == rec.row_off_host.tolist() and ring.cursors.tolist()[2] == 0
+        return batch, rec, q.contiguous(), kn.double(), vn.double()
+
+    prefix = torch.full((1, S // P), -1, dtype=torch.int32, device="cuda")
+    _, _, _, pk, pv = step(prefix, [0], [S])
+    table = torch.full((B, 8), -1, dtype=torch.int32, device="cuda")
+    shared = absb.SharedPrefix([0, B], [S], up([0, B]), up([S]))
+    table[:, :S // P] = prefix
+    have = [(pk, pv)] * B
+    lens = [S] * B
+    for after in ([S + 5, S + 20, S, S + 1], [S + 6, S, S + 17, S + 2], [S + 7, S, S + 18, S + 40], [S + 8, S + 33, S, S], [S, S + 34, S + 16, S + 1]):
+        batch, rec, q, kn, vn = step(table, lens, after)
+        # every page: free, the prefix's, or one request's
+        head, tail = ring.cursors.tolist()[:2]
+        free = [int(ring.pages[i % pages]) for i in range(head, tail)]
+        held = [int(x) for b in range(B) for x in table[b, S // P:-(-after[b] // P)]]
+        assert sorted(free + held + prefix[0].tolist()) == list(range(pages))
+        out = torch.empty_like(q)
+        lse = torch.empty((len(q), Hq), dtype=torch.float32, device="cuda")
+        ws = torch.zeros(absb.absb_attend_workspace(layer, batch, rec, shared), dtype=torch.uint8, device="cuda")
+        absb.absb_attend_shared(layer, batch, rec, shared, q, k, v, out, lse, None, ws)
+        torch.cuda.synchronize()
+        off = rec.row_off_host
+        for b in range(B):
+            r = slice(int(off[b]), int(off[b + 1]))
+            K, V = (torch.cat([old, new[r]]) if after[b] > lens[b] else old[:after[b]] for old, new in zip(have[b], (kn, vn)))
+            have[b] = (K, V)
+            for i in range(r.start, r.stop):
+                n = after[b] - (r.stop - 1 - i)
+                for h in range(Hq):
+                    s = (K[:n, h // 4] * q[i, h].double()).sum(1) / math.sqrt(D)
+                    w = torch.softmax(s, 0)[:, None]
+                    want, mag = (w * V[:n, h // 4]).sum(0), (w * V[:n, h // 4].abs()).sum(0)
+                    far = (out[i, h].double() - want).abs() - (STEP["f16"] * (mag + want.abs()) + 4e-5 * mag + 2.0 ** -24)
+                    assert float(far.max()) <= 0 and abs(float(lse[i, h]) - float(torch.logsumexp(s, 0))) <= 2.0 ** -16 + 1e-6 * float(s.abs().max())
+        lens = after
+    step(table, lens, [S] * B)
+    step(prefix, [S], [0])
+    head, tail = ring.cursors.tolist()[:2]
+    assert sorted(int(ring.pages[i % pages]) for i in range(head, tail)) == list(range(pages))
