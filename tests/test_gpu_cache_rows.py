@@ -952,3 +952,35 @@ def test_the_run_of_a_server_with_a_shared_prefix():
     step(prefix, [S], [0])
     head, tail = ring.cursors.tolist()[:2]
     assert sorted(int(ring.pages[i % pages]) for i in range(head, tail)) == list(range(pages))
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("rot,pairs", [(128, False), (64, False), (128, True), (40, True), (20, False)])
+@pytest.mark.parametrize("rows", [6007, 13001])
+def test_rotate_of_more_than_caches_keep(dt, rot, pairs, rows):
+    """70 and 152 MB of 48 heads, which pass the caches by on the way in, and out: the same bits as in stretches of 1000 rows."""
+    torch, absb = _torch(), _absb()
+    Hq, Hkv, P = 32, 8, 16
+    tdt = torch.float16 if dt == "f16" else torch.bfloat16
+    g = torch.Generator(device="cuda").manual_seed(rows + rot)
+    qkv = torch.randn((rows, (Hq + 2 * Hkv), D), generator=g, device="cuda").to(tdt)
+    q, k, v = qkv.split((Hq, Hkv, Hkv), 1)
+    pages = rows // P + 2
+    slot = torch.randperm(pages * P, generator=g, device="cuda")[:rows]
+    slot[::97] = -1
+    pos = torch.randint(0, 1 << 20, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    rope = absb.Rope(rot_dim=rot, layout=absb.ROPE_PAIRS if pairs else absb.ROPE_HALVES, base=500000.0)
+    freq = torch.from_numpy(absb.absb_rope_frequencies(rope)).cuda()
+    layer = _layer(Hq, Hkv, P, dt)
+    got, want = ([torch.full((rows, Hq, D), float("nan"), dtype=tdt, device="cuda")] +
+                 [torch.zeros((pages, Hkv, P, D), dtype=tdt, device="cuda") for _ in range(2)] for _ in range(2))
+    absb.absb_rotate_store(layer, rope, pos, slot, freq, q, got[0], k, v, got[1], got[2])
+    for a in range(0, rows, 1000):
+        b = min(a + 1000, rows)
+        absb.absb_rotate_store(layer, rope, pos[a:b], slot[a:b], freq, q[a:b], want[0][a:b], k[a:b], v[a:b], want[1], want[2])
+    torch.cuda.synchronize()
+    assert all(torch.equal(x.view(torch.int16), y.view(torch.int16)) for x, y in zip(got, want))
+    alone = q.contiguous()        # queries alone, in place
+    absb.absb_rotate_store(layer, rope, pos, None, freq, alone, alone)
+    torch.cuda.synchronize()
+    assert torch.equal(alone.view(torch.int16), got[0].view(torch.int16))
