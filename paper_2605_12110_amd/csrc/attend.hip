@@ -11,8 +11,9 @@
 //                rounded in pairs, are the operand P^T as they stand.  V^T comes from row-major V by the transposing read.
 //
 // Wide tiles, 128 rows: four waves of 32 go over the same keys, 64 at a time, so a key is read once for 128 rows; bound by the matrix
-// unit (32 query and 8 KV heads, f16: a prompt of 4 K 149 us, 920 TFLOP/s; 16 K 2180, 1010; chunks of 1 K behind 32 K 950) at
-// a clock that power holds at 1.55-1.6 GHz.  Two work-groups a compute unit: with one, 875 TFLOP/s at 16 K instead of 1036.
+// unit (32 query and 8 KV heads, f16: a prompt of 4 K 153 us, 895 TFLOP/s; 16 K 2180, 1010; a chunk of 1 K behind 32 K 970) at
+// a clock that power holds at 1.65 GHz.  Of 256 registers a lane, kernels with a cap and a bias spill 2, with a wide cap 6, with
+// that and a bias 4.  Two work-groups a compute unit: with one, 875 TFLOP/s at 16 K instead of 1036.
 // Narrow ones, 32 rows: four waves with keys of their own, none waiting for another; bound by memory (a token behind
 // 128 K 88 us, 6.1 TB/s).
 //

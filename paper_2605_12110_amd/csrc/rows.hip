@@ -176,8 +176,8 @@ __global__ __launch_bounds__(T) void map_rows_kernel(MapParams p) {
 
 int launch_map_rows(const MapParams& p, hipStream_t stream) {
   // Two rows a thread, and with a ring a work-group for every 64 requests, whose pages the host does not know; at most 192: the
-  // last one, who sets the cursors, hears from all the others one after the other (a step of 512 requests and 190000
-  // rows 9.0 us with 185, 9.5 with 256 or 93).
+  // last one, who sets the cursors, hears from all the others one after the other (a step of 512 requests and 302803
+  // rows 10.0 us with 192, 10.3 with 256, 10.6 with 96; of 151570 rows 8.65 with 148, 8.6 with 96, 8.9 with 74).
   const int threads = p.batch <= 256 ? 256 : p.batch <= 512 ? 512 : 1024;
   const int by_rows = p.max_rows <= 2 * threads ? 1 : p.max_rows / (2 * threads), by_pages = p.ring ? p.batch / 64 : 1;
   const int wgs = by_rows > by_pages ? by_rows : by_pages;
@@ -199,8 +199,8 @@ int launch_map_rows(const MapParams& p, hipStream_t stream) {
 // binary32 (2^-26 turns at most), to the hardware's sine and cosine of turns (off by at most 1.3e-7 over that range, where a 16-bit
 // result is off by 2^-12 at best).
 //
-// Bound by memory: (Hq + 2 Hkv) rows of 256 bytes in and out a token (8192 tokens of 48 heads 38.5 us, 32 K 140 us, 5.2 and 5.65 TB/s;
-// 16 tokens 4.0 us, a chain of round trips).  A lane holds 16-byte pieces (of both halves of a pair's
+// Bound by memory: (Hq + 2 Hkv) rows of 256 bytes in and out a token (8192 tokens of 48 heads 39 us, 32 K 140 us, 5.2 and 5.65 TB/s;
+// 16 tokens 3.9 us, a chain of round trips).  A lane holds 16-byte pieces (of both halves of a pair's
 // channels), LANES of them a head; a wave works on one token and a stretch of its heads, so that the sines are worked out once for
 // several heads.
 __device__ __forceinline__ uint64_t turns_of(double f) {
@@ -312,7 +312,7 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateParams p) {
 }
 
 // Any even rot_dim: a lane takes pair `lane` of a head (two channels apart by any distance) and, behind the pairs, channels
-// that pass two by two.
+// that pass two by two.  Two bytes a lane, a head after the other: 8192 tokens of 48 heads 66 us, 3.1 TB/s.
 template <int DT>
 __global__ __launch_bounds__(256) void rotate_any_kernel(RotateParams p) {
   const int task = (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
