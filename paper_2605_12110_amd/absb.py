@@ -452,10 +452,11 @@ class SharedPrefix(_Record):
     def _make(self):
         a, a_at = _i32_host(self.first_host)
         n, n_at = _i32_host(self.len_host)
-        if len(a) != len(n) + 1:
+        groups = 0 if n is None else len(n)
+        if a is not None and n is not None and len(a) != groups + 1:
             raise AbsbError(ERR_BAD_SHAPE, "absb_shared_prefix")
-        rec = _Shared(len(n), a_at, n_at, _dense(self.first, 4 * len(a), "absb_shared_prefix"),
-                      _dense(self.length, 4 * len(n), "absb_shared_prefix"))
+        rec = _Shared(groups, a_at, n_at, _dense(self.first, 4 * groups + 4, "absb_shared_prefix"),
+                      _dense(self.length, 4 * groups, "absb_shared_prefix"))
         rec._arrays = (a, n)
         return rec
 

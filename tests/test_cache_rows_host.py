@@ -332,3 +332,8 @@ def test_rotate_and_map_refuse_tensors_shorter_than_the_step():
         d.update(kw)
         _refused(absb.ERR_BAD_SHAPE, absb.absb_map_rows, _layer(), batch, *d.values())
     _refused(absb.ERR_BAD_SHAPE, absb.absb_map_rows, *_map(batch=batch, ring=ring()), cursors_out=_zeros(3, dtype=i64))
+
+
+@pytest.mark.parametrize("shared", [absb.SharedPrefix(None, [64], AT, AT), absb.SharedPrefix([0, 2], None, AT, AT)])
+def test_attend_shared_without_its_host_arrays(shared):
+    _refused(absb.ERR_NULL, absb.absb_attend_shared, _layer(), _batch((100, 200)), _rows((1, 2)), shared, AT, AT, AT, AT, None, None, BIG_WS)
