@@ -984,3 +984,18 @@ def test_rotate_of_more_than_caches_keep(dt, rot, pairs, rows):
     absb.absb_rotate_store(layer, rope, pos, None, freq, alone, alone)
     torch.cuda.synchronize()
     assert torch.equal(alone.view(torch.int16), got[0].view(torch.int16))
+
+
+@pytest.mark.parametrize("lens,new", [([700], [600]), ([4000], [4])])
+def test_attend_of_weights_below_the_normal_values_of_f16(lens, new):
+    """As above, with one key in 256 whose weight is 1 and the others' 2^-14 to 2^-18: products and sums both keep them."""
+    torch = _torch()
+    c = Call(lens, new, 8, 2, 16, "f16", seed=7)
+    t = np.arange(lens[0])
+    page, slot = torch.from_numpy(c.table_host[0, t // 16].astype(np.int64)).cuda(), torch.from_numpy(t % 16).cuda()
+    c.view(c.k)[page, :, slot] = torch.from_numpy((t % 256 == 0) * 1.0).cuda().half()[:, None, None]
+    c.q[:] = torch.linspace(14 / 16.32, 18 / 16.32, c.rows * c.Hq, device="cuda").view(c.rows, c.Hq, 1).half()   # sqrt(128) log2(e) = 16.32
+    value = (1.0 + torch.arange(D, device="cuda") / 128.0).half()
+    c.view(c.v)[:] = torch.where(torch.isinf(c.view(c.v)), c.view(c.v), value)
+    c.check(f"{lens} {new}")
+    assert torch.equal(c.out[:c.rows], value.expand(c.rows, c.Hq, D))
