@@ -497,7 +497,7 @@ ABSB_API int absb_rotate_store(const absb_layer* layer, const absb_rope* rope, i
  * set).  All zero and NULL: causal attention.  A row that sees nothing yields out = 0, lse = -inf.  The cap is off by at most
  * 3 * 2^-23 softcap for caps up to 64, by 2^-19 of the capped score for wider ones. */
 typedef struct absb_score_opts {
-  float softcap;              /* 0 = none, else 1e-30 to 1e30                                    */
+  float softcap;              /* 0 = none, else 1e-30 to 1e30; 3 sm_scale / softcap, as 1.5 sm_scale, is below 2^128 */
   int32_t window;             /* 0 = none, else >= 1: tokens a row sees up to and including itself      */
   const float* slopes;        /* device [Hq] or NULL                                             */
   const int32_t* prefix_lens; /* device [Bt] or NULL: tokens that all rows of a request see            */

@@ -986,6 +986,7 @@ static int attend(const absb_layer* layer, const absb_batch* batch, const absb_r
     p.cap_log2 = cap * 1.4426950408889634f;
     p.cap_in = scale / cap * 2.8853900817779268f;
   }
+  if (std::isinf(p.scale_log2) || std::isinf(p.cap_in)) return ABSB_ERR_BAD_SHAPE;  // (a score of 0 would be NaN)
   return launch_attend(p, plan, layer->dtype, cap, static_cast<hipStream_t>(stream));
 }
 

@@ -337,3 +337,9 @@ def test_rotate_and_map_refuse_tensors_shorter_than_the_step():
 @pytest.mark.parametrize("shared", [absb.SharedPrefix(None, [64], AT, AT), absb.SharedPrefix([0, 2], None, AT, AT)])
 def test_attend_shared_without_its_host_arrays(shared):
     _refused(absb.ERR_NULL, absb.absb_attend_shared, _layer(), _batch((100, 200)), _rows((1, 2)), shared, AT, AT, AT, AT, None, None, BIG_WS)
+
+
+@pytest.mark.parametrize("scale,cap", [(1e9, 1e-30), (3e38, 0.0), (3e38, 1e30)])
+def test_attend_refuses_scales_that_binary32_does_not_hold(scale, cap):
+    """sm_scale log2(e), and 2 log2(e) sm_scale / cap: infinite, times a score of 0."""
+    _refused(absb.ERR_BAD_SHAPE, absb.absb_attend_rows, *_att(layer=_layer(sm_scale=scale), opts=absb.ScoreOpts(softcap=cap), ws=BIG_WS))
